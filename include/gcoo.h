@@ -284,6 +284,94 @@ int gcoo_set_share_policy(int policy);
 int gcoo_export_share(const gcoo_matrix* A, uint32_t* hdr, uint32_t* blocks, int32_t* sbase, int32_t* ucount, int32_t* ucols,
                       int64_t* hdr_words, int64_t* block_count, void* stream);
 
+/*
+ * A layer with sparse weights: C = act(A x B + bias) + residual, its gradients, and the clipping of them.
+ *
+ * A holds the weights of such a layer (fp32, as everywhere here), B has a column per token.  The dense matrices that a layer passes on are fp32,
+ * bfloat16 or float16, one type for all matrices of a call; bias, the gradients of the bias and of the weights, and every sum are fp32, and
+ * a result is rounded once, to nearest even, when it is stored.  Matrices are row-major on the device, aligned to their element type, with
+ * leading dimensions in elements; any alignment beyond that is served (rows and leading dimensions at multiples of 16 bytes are the fastest).
+ *
+ * These calls launch kernels on `stream` and return, like gcoo_spdm(): they wait for nothing, allocate nothing, copy nothing back and may be recorded into a
+ * stream capture.  Results are the same bits from run to run.  `work` is device memory of the caller (256-byte aligned, at least as many bytes as the
+ * function named beside it says for the same arguments; NULL where that is 0), free to be used again once the call's kernels have finished: two calls
+ * that overlap in time, and two captured graphs that may be replayed at the same time, need work of their own.
+ */
+#define GCOO_F32  0
+#define GCOO_BF16 1
+#define GCOO_F16  2
+
+#define GCOO_ACT_NONE      0
+#define GCOO_ACT_RELU      1   /* max(z, 0) */
+#define GCOO_ACT_SILU      2   /* z / (1 + exp(-z)) */
+#define GCOO_ACT_GELU      3   /* z Phi(z), Phi the distribution function of N(0,1) */
+#define GCOO_ACT_GELU_TANH 4   /* z / (1 + exp(-2u)), u = sqrt(2/pi) (z + 0.044715 z^3) */
+
+/* What follows the product.  All zero: C = A x B in fp32. */
+typedef struct gcoo_epilogue {
+    int32_t type;            /* GCOO_F32, GCOO_BF16 or GCOO_F16: of B, residual, Z and C */
+    int32_t activation;      /* GCOO_ACT_* */
+    const float* bias;       /* m, one for each row of C, or NULL */
+    const void* residual;    /* m x N, leading dimension ldr >= N, or NULL; may be C itself (then ldr == ldc) */
+    int64_t ldr;
+    void* Z;                 /* m x N, leading dimension ldz >= N: receives A x B + bias, what gcoo_epilogue_grad() needs; or NULL */
+    int64_t ldz;
+} gcoo_epilogue;
+
+/*
+ * C = act(A x B + bias) + residual.  B (k x N, ldb >= N), C (m x N, ldc >= N).  Neither C nor Z may overlap B, bias or each other, nor the residual but for C as
+ * the residual itself.  The activation takes the sum in fp32, not what Z holds of it.  A row of A without entries gives Z = bias.  A row of B
+ * that no stored entry touches does not reach C.  N = 0 or m = 0 is a no-op success.
+ * GCOO_EINVAL for an unknown type or activation, a leading dimension below N or, for B, of 2^30 elements and more, a base address that is no multiple of the
+ * element size, a missing pointer; GCOO_ENOMEM where work_bytes is too small.
+ * The gradient of B is this product with the transpose of A: gcoo_spdm_epilogue(At, dZ, ..., dB).
+ */
+size_t gcoo_spdm_epilogue_bytes(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int64_t N, const gcoo_epilogue* e, const void* C_dev, int64_t ldc);
+int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int64_t N, const gcoo_epilogue* e, void* C_dev, int64_t ldc,
+                       void* work, size_t work_bytes, void* stream);
+
+/*
+ * The gradient through the epilogue: dZ = dC act'(Z) (m x N), dbias[i] = the sum of row i of dZ before it is rounded to the type.
+ *   Z_dev     m x N, ldz >= N: what gcoo_spdm_epilogue() stored; NULL for GCOO_ACT_NONE, where it is not read
+ *   dC_dev    m x N, lddc >= N: the gradient of C, which is the gradient of the residual as well
+ *   dZ_dev    m x N, lddz >= N, or NULL where only dbias is wanted; may be dC itself (then lddz == lddc)
+ *   dbias_dev m, or NULL
+ * relu has the slope 0 at 0.  m = 0 is a no-op success, N = 0 gives dbias = 0.
+ */
+size_t gcoo_epilogue_grad_bytes(int64_t m, int64_t N);
+int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const void* Z_dev, int64_t ldz, const void* dC_dev, int64_t lddc,
+                       void* dZ_dev, int64_t lddz, float* dbias_dev, void* work, size_t work_bytes, void* stream);
+
+/*
+ * The gradient of the stored weights: dvals[e] = the sum over n of dZ(row of e, n) B(column of e, n), for every stored entry e of A and for no other.
+ *   dZ_dev    m x N, lddz >= N;  B_dev  k x N, ldb >= N, both of `type`
+ *   dvals_dev nnz, in row order: row by row, and in a row as the entries came (of a CSR input the order of its `vals`, of a dense input ascending columns)
+ * An entry that is stored twice has the same gradient in both places.  N = 0 gives zeros.  GCOO_EINVAL as for gcoo_spdm_epilogue(), the limit of 2^30 for
+ * both leading dimensions.
+ */
+size_t gcoo_spdm_grad_values_bytes(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type);
+int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type,
+                          float* dvals_dev, void* work, size_t work_bytes, void* stream);
+
+/* One of the tensors whose gradients are clipped: `count` adjacent elements. */
+typedef struct gcoo_gradient {
+    const void* data;
+    void* out;               /* receives the scaled elements; data itself: in place */
+    int64_t count;           /* >= 0 */
+    int32_t type;            /* GCOO_F32, GCOO_BF16 or GCOO_F16, of data and of out */
+} gcoo_gradient;
+
+/*
+ * norm = sqrt(the sum of the squares of all elements of all tensors); out = data x min(1, max_norm / (norm + 1e-6)).
+ * Squares and their sums are held in 64 bits.  Where the factor is 1, tensors in place are left as they are.  Elements that are not finite make the norm
+ * not finite: an infinite one makes the factor 0, NaN makes every element NaN.  max_norm = INFINITY (or above any norm) copies what is not in place.
+ *   list      `tensors` of them in HOST memory, read before the call returns; a range of `out` may overlap no range of another tensor, nor its own `data` but
+ *             as data itself (GCOO_EINVAL)
+ *   norm_dev  receives the norm (fp32, device)
+ */
+size_t gcoo_clip_grad_norm_bytes(const gcoo_gradient* list, int64_t tensors);
+int gcoo_clip_grad_norm(const gcoo_gradient* list, int64_t tensors, float max_norm, float* norm_dev, void* work, size_t work_bytes, void* stream);
+
 /* Static text for a status code. */
 const char* gcoo_strerror(int status);
 

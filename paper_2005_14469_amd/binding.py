@@ -27,19 +27,35 @@ GCOO_MAX_P = 256
 VARIANT_AUTO, VARIANT_LDS, VARIANT_REG, VARIANT_SHARE = 0, 1, 2, 3
 KERNEL_NONE, KERNEL_LDS, KERNEL_SCHED, KERNEL_SHARE, KERNEL_ROWS, KERNEL_BAND = 0, 1, 2, 3, 4, 5
 SHARE_AUTO, SHARE_ALWAYS, SHARE_NEVER = 0, 1, 2
+GCOO_F32, GCOO_BF16, GCOO_F16 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
+ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH}
+_TYPES = {torch.float32: GCOO_F32, torch.bfloat16: GCOO_BF16, torch.float16: GCOO_F16}
 
 # every symbol include/gcoo.h declares
 SYMBOLS = ["gcoo_default_p", "gcoo_device_bytes", "gcoo_from_csr", "gcoo_from_csr_device", "gcoo_dense_nnz", "gcoo_from_dense", "gcoo_spdm",
            "gcoo_dense_count_bytes", "gcoo_dense_count", "gcoo_from_dense_counted",
            "gcoo_spdm_variant", "gcoo_spdm_pick", "gcoo_spdm_kernel", "gcoo_free", "gcoo_info", "gcoo_export",
            "gcoo_strerror", "gcoo_last_hip_error", "gcoo_set_share_policy", "gcoo_export_share",
-           "gcoo_static_handle_bytes", "gcoo_from_csr_device_static"]
+           "gcoo_static_handle_bytes", "gcoo_from_csr_device_static",
+           "gcoo_spdm_epilogue_bytes", "gcoo_spdm_epilogue", "gcoo_epilogue_grad_bytes", "gcoo_epilogue_grad",
+           "gcoo_spdm_grad_values_bytes", "gcoo_spdm_grad_values", "gcoo_clip_grad_norm_bytes", "gcoo_clip_grad_norm"]
 # and include/gcoo_baseline.h (libgcoo_baseline.so)
 BASELINE_SYMBOLS = ["gcoo_csr_spmm_baseline"]
 
 _lib = None
 _calls = None              # the extension module, or what stands for it: there as soon as lib() has been called
 _baseline_lib = None
+
+
+class Epilogue(C.Structure):
+    """gcoo_epilogue"""
+    _fields_ = [("type", C.c_int32), ("activation", C.c_int32), ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64), ("Z", C.c_void_p), ("ldz", C.c_int64)]
+
+
+class Gradient(C.Structure):
+    """gcoo_gradient"""
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("type", C.c_int32)]
 
 
 class GcooError(RuntimeError):
@@ -110,6 +126,23 @@ def lib():
         L.gcoo_static_handle_bytes.argtypes = [i64, i64, i64, i32]
         L.gcoo_from_csr_device_static.restype = C.c_int
         L.gcoo_from_csr_device_static.argtypes = [i64, i64, i64, vp, vp, vp, i32, vp, C.c_size_t, vp, C.POINTER(vp)]
+        ep, gp = C.POINTER(Epilogue), C.POINTER(Gradient)
+        L.gcoo_spdm_epilogue_bytes.restype = sz
+        L.gcoo_spdm_epilogue_bytes.argtypes = [vp, vp, i64, i64, ep, vp, i64]
+        L.gcoo_spdm_epilogue.restype = C.c_int
+        L.gcoo_spdm_epilogue.argtypes = [vp, vp, i64, i64, ep, vp, i64, vp, sz, vp]
+        L.gcoo_epilogue_grad_bytes.restype = sz
+        L.gcoo_epilogue_grad_bytes.argtypes = [i64, i64]
+        L.gcoo_epilogue_grad.restype = C.c_int
+        L.gcoo_epilogue_grad.argtypes = [i64, i64, C.c_int, C.c_int, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.gcoo_spdm_grad_values_bytes.restype = sz
+        L.gcoo_spdm_grad_values_bytes.argtypes = [vp, vp, i64, vp, i64, i64, C.c_int]
+        L.gcoo_spdm_grad_values.restype = C.c_int
+        L.gcoo_spdm_grad_values.argtypes = [vp, vp, i64, vp, i64, i64, C.c_int, vp, vp, sz, vp]
+        L.gcoo_clip_grad_norm_bytes.restype = sz
+        L.gcoo_clip_grad_norm_bytes.argtypes = [gp, i64]
+        L.gcoo_clip_grad_norm.restype = C.c_int
+        L.gcoo_clip_grad_norm.argtypes = [gp, i64, C.c_float, vp, vp, sz, vp]
         L.gcoo_set_share_policy.restype = C.c_int
         L.gcoo_set_share_policy.argtypes = [C.c_int]
         L.gcoo_export_share.restype = C.c_int
@@ -184,6 +217,7 @@ class GcooMatrix:
         self._h = handle.value if isinstance(handle, C.c_void_p) else handle          # the address: what the extension module takes
         self.buf = buf
         self._mk = None
+        self._nnz = None
 
     @property
     def shape(self):
@@ -191,6 +225,12 @@ class GcooMatrix:
             i = self.info()
             self._mk = (i["m"], i["k"])
         return self._mk
+
+    @property
+    def nnz(self) -> int:
+        if self._nnz is None:
+            self._nnz = self.info()["nnz"]
+        return self._nnz
 
     def _address(self) -> int:
         if self._h is None:
@@ -438,6 +478,142 @@ def gcoo_spdm_pick(A: GcooMatrix, B: torch.Tensor, C_out: torch.Tensor) -> int:
 def gcoo_spdm_kernel(A: GcooMatrix, B: torch.Tensor, C_out: torch.Tensor, variant: int = VARIANT_AUTO) -> int:
     """The kernel (KERNEL_*) that gcoo_spdm() launches for these arguments, or the negative status it fails with."""
     return int(lib().gcoo_spdm_kernel(A.handle, B.data_ptr(), B.stride(0), B.shape[1], C_out.data_ptr(), C_out.stride(0), variant))
+
+
+# ---- a layer with sparse weights ----
+
+def _activation(a) -> int:
+    if isinstance(a, str):
+        if a not in ACTIVATIONS:
+            raise ValueError(f"unknown activation {a!r}: one of {', '.join(ACTIVATIONS)}")
+        return ACTIVATIONS[a]
+    return int(a)
+
+
+def _rows_of(t: torch.Tensor, rows: int, N: int, dtype, d: int) -> int:
+    """The leading dimension of a dense rows x N matrix of adjacent elements, on device d."""
+    assert t.is_cuda and t.get_device() == d and t.dtype is dtype and t.shape == (rows, N) and (N <= 1 or t.stride(1) == 1)
+    return t.stride(0) if rows > 1 else max(N, 1)
+
+
+def _work(nbytes: int, device, stream):
+    """Memory for a call, which goes back to torch's pool behind it: its address (None for 0 bytes), and its owner."""
+    if nbytes == 0:
+        return None, None
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is not None:
+        _used_on(buf, stream)
+    return buf.data_ptr(), buf
+
+
+def gcoo_spdm_epilogue(A: GcooMatrix, B: torch.Tensor, bias: torch.Tensor | None = None, activation=ACT_NONE, residual: torch.Tensor | None = None,
+                       C_out: torch.Tensor | None = None, Z_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """C = act(A x B + bias) + residual on the current stream; Z_out, where given, receives A x B + bias.
+
+    B [k, N], residual, C_out and Z_out [m, N]: fp32, bfloat16 or float16, one type, unit column stride; bias [m] fp32; activation: ACT_* or a name of
+    ACTIVATIONS.  C_out may be the residual.  The gradient of B is the same call with the transpose of A."""
+    assert B.is_cuda and B.dim() == 2 and B.dtype in _TYPES
+    m, k = A.shape
+    N, d = B.shape[1], B.get_device()
+    A._address()
+    assert A.buf.get_device() == d
+    e = Epilogue(_TYPES[B.dtype], _activation(activation))
+    ldb = _rows_of(B, k, N, B.dtype, d)
+    if bias is not None:
+        assert bias.is_cuda and bias.get_device() == d and bias.dtype is torch.float32 and bias.shape == (m,) and (m <= 1 or bias.stride(0) == 1)
+        e.bias = bias.data_ptr()
+    if residual is not None:
+        e.ldr, e.residual = _rows_of(residual, m, N, B.dtype, d), residual.data_ptr()
+    if Z_out is not None:
+        e.ldz, e.Z = _rows_of(Z_out, m, N, B.dtype, d), Z_out.data_ptr()
+    L = lib()
+    with _on(d):
+        if C_out is None:
+            C_out = torch.empty((m, N), dtype=B.dtype, device=B.device)
+        ldc = _rows_of(C_out, m, N, B.dtype, d)
+        need = L.gcoo_spdm_epilogue_bytes(A.handle, B.data_ptr(), ldb, N, C.byref(e), C_out.data_ptr(), ldc)
+        work, _keep = _work(need, B.device, stream)
+        if stream is not None:
+            for t in (A.buf, B, bias, residual, C_out, Z_out):
+                if t is not None:
+                    _used_on(t, stream)
+        _check(L.gcoo_spdm_epilogue(A.handle, B.data_ptr(), ldb, N, C.byref(e), C_out.data_ptr(), ldc, work, need, _stream_ptr(stream)), "gcoo_spdm_epilogue")
+    return C_out
+
+
+def gcoo_epilogue_grad(dC: torch.Tensor, Z: torch.Tensor | None = None, activation=ACT_NONE, dZ_out: torch.Tensor | None = None, stream=None):
+    """(dZ, dbias) of C = act(Z) + residual, Z = A x B + bias, from the gradient of C: dZ [m, N] of dC's type, dbias [m] fp32.
+
+    Z: what gcoo_spdm_epilogue() stored in Z_out; not needed without an activation, where dZ is dC (and is returned as dC itself unless dZ_out is given).
+    dZ_out may be dC."""
+    assert dC.is_cuda and dC.dim() == 2 and dC.dtype in _TYPES
+    (m, N), d, act = dC.shape, dC.get_device(), _activation(activation)
+    lddc = _rows_of(dC, m, N, dC.dtype, d)
+    assert Z is not None or act == ACT_NONE
+    ldz = 0 if act == ACT_NONE else _rows_of(Z, m, N, dC.dtype, d)
+    L = lib()
+    with _on(d):
+        if dZ_out is None and act != ACT_NONE:
+            dZ_out = torch.empty((m, N), dtype=dC.dtype, device=dC.device)
+        dbias = torch.empty(m, dtype=torch.float32, device=dC.device)
+        lddz = 0 if dZ_out is None else _rows_of(dZ_out, m, N, dC.dtype, d)
+        need = L.gcoo_epilogue_grad_bytes(m, N)
+        work, _keep = _work(need, dC.device, stream)
+        if stream is not None:
+            for t in (dC, Z, dZ_out, dbias):
+                if t is not None:
+                    _used_on(t, stream)
+        _check(L.gcoo_epilogue_grad(m, N, _TYPES[dC.dtype], act, None if act == ACT_NONE else Z.data_ptr(), ldz, dC.data_ptr(), lddc,
+                                    None if dZ_out is None else dZ_out.data_ptr(), lddz, dbias.data_ptr(), work, need, _stream_ptr(stream)), "gcoo_epilogue_grad")
+    return (dC if dZ_out is None else dZ_out), dbias
+
+
+def gcoo_spdm_grad_values(A: GcooMatrix, dZ: torch.Tensor, B: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient of the stored values of A, from that of Z = A x B: [nnz] fp32, in the order of the CSR arrays that A came from (of a dense A: row by row)."""
+    assert dZ.is_cuda and B.is_cuda and dZ.dim() == 2 and B.dim() == 2 and B.dtype in _TYPES
+    m, k = A.shape
+    N, d = B.shape[1], B.get_device()
+    A._address()
+    assert A.buf.get_device() == d
+    lddz, ldb, nnz = _rows_of(dZ, m, N, B.dtype, d), _rows_of(B, k, N, B.dtype, d), A.nnz
+    L = lib()
+    with _on(d):
+        if out is None:
+            out = torch.empty(nnz, dtype=torch.float32, device=B.device)
+        assert out.is_cuda and out.get_device() == d and out.dtype is torch.float32 and out.shape == (nnz,) and (nnz <= 1 or out.stride(0) == 1)
+        need = L.gcoo_spdm_grad_values_bytes(A.handle, dZ.data_ptr(), lddz, B.data_ptr(), ldb, N, _TYPES[B.dtype])
+        work, _keep = _work(need, B.device, stream)
+        if stream is not None:
+            for t in (A.buf, dZ, B, out):
+                _used_on(t, stream)
+        _check(L.gcoo_spdm_grad_values(A.handle, dZ.data_ptr(), lddz, B.data_ptr(), ldb, N, _TYPES[B.dtype], out.data_ptr(), work, need, _stream_ptr(stream)),
+               "gcoo_spdm_grad_values")
+    return out
+
+
+def gcoo_clip_grad_norm(tensors, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """Scales the tensors so that the norm over all of them is at most max_norm, and returns the norm that they had (fp32, on the device).
+
+    In place, or into `out`, as many contiguous tensors of the same shapes and types."""
+    tensors = list(tensors)
+    out = tensors if out is None else list(out)
+    assert tensors and len(out) == len(tensors)
+    d = tensors[0].get_device()
+    arr = (Gradient * len(tensors))()
+    for g, t, o in zip(arr, tensors, out):
+        assert t.is_cuda and t.get_device() == d and t.dtype in _TYPES and t.is_contiguous()
+        assert o.is_cuda and o.get_device() == d and o.dtype is t.dtype and o.shape == t.shape and o.is_contiguous()
+        g.data, g.out, g.count, g.type = t.data_ptr(), o.data_ptr(), t.numel(), _TYPES[t.dtype]
+    L = lib()
+    with _on(d):
+        norm = torch.empty((), dtype=torch.float32, device=tensors[0].device)
+        need = L.gcoo_clip_grad_norm_bytes(arr, len(tensors))
+        work, _keep = _work(need, norm.device, stream)
+        if stream is not None:
+            for t in (*tensors, *out, norm):
+                _used_on(t, stream)
+        _check(L.gcoo_clip_grad_norm(arr, len(tensors), max_norm, norm.data_ptr(), work, need, _stream_ptr(stream)), "gcoo_clip_grad_norm")
+    return norm
 
 
 def gcoo_csr_spmm_baseline(m: int, k: int, row_ptr: torch.Tensor, col_idx: torch.Tensor, vals: torch.Tensor,

@@ -23,6 +23,7 @@
 #include "gcoo_band.hpp"
 #include "gcoo_band_build.hpp"
 #include "gcoo_build_kernels.hpp"
+#include "gcoo_layer.hpp"
 #include "gcoo_order_kernels.hpp"
 #include "gcoo_sched.hpp"
 #include "gcoo_sched_build.hpp"
@@ -1779,3 +1780,14 @@ const char* gcoo_strerror(int status)
 const char* gcoo_last_hip_error(void) { return g_hip_error.c_str(); }
 
 }  // extern "C"
+
+namespace gcoo {
+
+RowsView rows_view(const gcoo_matrix* A)
+{
+    if (A->inner) A = A->inner;
+    return {A->m, A->k, A->nnz, A->row_start(), A->row_cols(), A->row_vals()};
+}
+int hip_failed(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+}  // namespace gcoo

@@ -1,0 +1,244 @@
+// Host side of the operators of a sparse layer (include/gcoo.h): argument checks, workspaces and launches.
+#include "gcoo_layer.hpp"
+#include "gcoo_layer_clip.hpp"
+
+#include <algorithm>
+#include <memory>
+#include <new>
+
+namespace {
+
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+bool known_type(int type) { return type == GCOO_F32 || type == GCOO_BF16 || type == GCOO_F16; }
+bool known_activation(int act) { return act >= GCOO_ACT_NONE && act <= GCOO_ACT_GELU_TANH; }
+bool on_elements(const void* p, int type) { return reinterpret_cast<uintptr_t>(p) % gcoo::type_bytes(type) == 0; }
+bool on_floats(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+constexpr int64_t kMaxPitch = 0x3fffffff;
+
+int check_work(const void* work, size_t given, size_t need)
+{
+    if (need == 0) return GCOO_OK;
+    if (given < need) return GCOO_ENOMEM;
+    return work && reinterpret_cast<uintptr_t>(work) % 256 == 0 ? GCOO_OK : GCOO_EINVAL;
+}
+int done(hipError_t e, const char* what) { return e == hipSuccess ? GCOO_OK : gcoo::hip_failed(e, what); }
+
+// ---- the product with its epilogue ----
+
+int check_product(const gcoo::RowsView& A, const void* B, int64_t ldb, int64_t N, const gcoo_epilogue* e, const void* C, int64_t ldc)
+{
+    if (!e || !known_type(e->type) || !known_activation(e->activation)) return GCOO_EINVAL;
+    if (N < 0 || N > INT32_MAX || ldb < N || ldb > kMaxPitch || ldc < N) return GCOO_EINVAL;
+    if ((e->residual && e->ldr < N) || (e->Z && e->ldz < N)) return GCOO_EINVAL;
+    if (!on_elements(B, e->type) || !on_elements(C, e->type) || !on_elements(e->residual, e->type) || !on_elements(e->Z, e->type) || !on_floats(e->bias)) return GCOO_EINVAL;
+    if (N == 0 || A.m == 0) return GCOO_OK;
+    if (!C || (A.nnz > 0 && !B)) return GCOO_EINVAL;
+    if (e->residual == C && e->residual && e->ldr != ldc) return GCOO_EINVAL;
+    if (e->Z == C) return GCOO_EINVAL;
+    return GCOO_OK;
+}
+
+// B in fp32 where it is not, and the product in front of the epilogue.
+struct ProductPlan { size_t wide_b, product, total; int64_t ldw; };
+ProductPlan product_plan(const gcoo::RowsView& A, int64_t N, int type)
+{
+    ProductPlan p{0, 0, 0, (N + 31) / 32 * 32};
+    if (A.nnz == 0 || A.m == 0 || N == 0) return p;
+    if (type != GCOO_F32) { p.wide_b = 0; p.total += aligned((size_t)A.k * (size_t)p.ldw * 4); }
+    p.product = p.total;
+    p.total += aligned((size_t)A.m * (size_t)p.ldw * 4);
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gcoo_spdm_epilogue_bytes(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int64_t N, const gcoo_epilogue* e, const void* C_dev, int64_t ldc)
+{
+    if (!A) return 0;
+    const gcoo::RowsView v = gcoo::rows_view(A);
+    return check_product(v, B_dev, ldb, N, e, C_dev, ldc) == GCOO_OK ? product_plan(v, N, e->type).total : 0;
+}
+
+int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int64_t N, const gcoo_epilogue* e, void* C_dev, int64_t ldc,
+                       void* work, size_t work_bytes, void* stream)
+{
+    if (!A) return GCOO_EINVAL;
+    const gcoo::RowsView v = gcoo::rows_view(A);
+    int rc = check_product(v, B_dev, ldb, N, e, C_dev, ldc);
+    if (rc != GCOO_OK || N == 0 || v.m == 0) return rc;
+    const ProductPlan plan = product_plan(v, N, e->type);
+    rc = check_work(work, work_bytes, plan.total);
+    if (rc != GCOO_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const gcoo::EpilogueArgs args{e->bias, e->residual, e->ldr, e->Z, e->ldz, C_dev, ldc, e->type, e->activation};
+    if (v.nnz == 0) return done(gcoo::launch_epilogue(nullptr, 0, v.m, N, args, s), "layer_epilogue launch");
+    float* P = reinterpret_cast<float*>(static_cast<char*>(work) + plan.product);
+    const float* B = static_cast<const float*>(B_dev);
+    if (e->type != GCOO_F32) {
+        float* W = reinterpret_cast<float*>(static_cast<char*>(work) + plan.wide_b);
+        rc = done(gcoo::launch_widen(B_dev, ldb, e->type, W, plan.ldw, v.k, N, s), "layer_widen launch");
+        if (rc != GCOO_OK) return rc;
+        B = W;
+        ldb = plan.ldw;
+    }
+    rc = gcoo_spdm(A, B, ldb, N, P, plan.ldw, stream);
+    return rc != GCOO_OK ? rc : done(gcoo::launch_epilogue(P, plan.ldw, v.m, N, args, s), "layer_epilogue launch");
+}
+
+size_t gcoo_epilogue_grad_bytes(int64_t m, int64_t N)
+{
+    (void)m; (void)N;
+    return 0;
+}
+
+int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const void* Z_dev, int64_t ldz, const void* dC_dev, int64_t lddc,
+                       void* dZ_dev, int64_t lddz, float* dbias_dev, void* work, size_t work_bytes, void* stream)
+{
+    if (m < 0 || N < 0 || m > INT32_MAX || N > INT32_MAX || !known_type(type) || !known_activation(activation)) return GCOO_EINVAL;
+    if (lddc < N || (dZ_dev && lddz < N) || !on_elements(dC_dev, type) || !on_elements(dZ_dev, type) || !on_floats(dbias_dev)) return GCOO_EINVAL;
+    const bool reads_z = activation != GCOO_ACT_NONE;
+    if (reads_z && (ldz < N || !on_elements(Z_dev, type))) return GCOO_EINVAL;
+    if (m == 0) return GCOO_OK;
+    if (N > 0 && (!dC_dev || (reads_z && !Z_dev))) return GCOO_EINVAL;
+    if (dZ_dev && dZ_dev == dC_dev && lddz != lddc) return GCOO_EINVAL;
+    const int rc = check_work(work, work_bytes, gcoo_epilogue_grad_bytes(m, N));
+    if (rc != GCOO_OK || (!dbias_dev && (!dZ_dev || N == 0))) return rc;
+    const gcoo::EpilogueGradArgs a{Z_dev, ldz, dC_dev, lddc, dZ_dev, lddz, dbias_dev, m, N, type, activation};
+    return done(gcoo::launch_epilogue_grad(a, static_cast<hipStream_t>(stream)), "layer_epilogue_grad launch");
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_values(const gcoo::RowsView& A, const void* dZ, int64_t lddz, const void* B, int64_t ldb, int64_t N, int type)
+{
+    if (!known_type(type) || N < 0 || N > INT32_MAX || lddz < N || ldb < N || lddz > kMaxPitch || ldb > kMaxPitch) return GCOO_EINVAL;
+    if (!on_elements(dZ, type) || !on_elements(B, type)) return GCOO_EINVAL;
+    return N > 0 && A.nnz > 0 && (!dZ || !B) ? GCOO_EINVAL : GCOO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gcoo_spdm_grad_values_bytes(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type)
+{
+    if (!A || check_values(gcoo::rows_view(A), dZ_dev, lddz, B_dev, ldb, N, type) != GCOO_OK) return 0;
+    return 0;
+}
+
+int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type,
+                          float* dvals_dev, void* work, size_t work_bytes, void* stream)
+{
+    if (!A) return GCOO_EINVAL;
+    const gcoo::RowsView v = gcoo::rows_view(A);
+    int rc = check_values(v, dZ_dev, lddz, B_dev, ldb, N, type);
+    if (rc != GCOO_OK) return rc;
+    if (!on_floats(dvals_dev) || (v.nnz > 0 && !dvals_dev)) return GCOO_EINVAL;
+    if (v.nnz == 0) return GCOO_OK;
+    rc = check_work(work, work_bytes, 0);
+    if (rc != GCOO_OK) return rc;
+    const gcoo::GradValuesArgs a{v, dZ_dev, lddz, B_dev, ldb, N, type, dvals_dev};
+    return done(gcoo::launch_grad_values(a, static_cast<hipStream_t>(stream)), "layer_values launch");
+}
+
+}  // extern "C"
+
+// ---- clipping ----
+
+namespace {
+
+int64_t clip_pieces(int64_t count) { return (count + gcoo::kClipPiece - 1) / gcoo::kClipPiece; }
+
+// The number of pieces of all tensors, or a status.
+int64_t check_clip(const gcoo_gradient* list, int64_t tensors)
+{
+    if (tensors < 0 || tensors > INT32_MAX || (tensors > 0 && !list)) return GCOO_EINVAL;
+    int64_t pieces = 0;
+    for (int64_t i = 0; i < tensors; ++i) {
+        const gcoo_gradient& t = list[i];
+        if (!known_type(t.type) || t.count < 0 || t.count > INT64_MAX / 8) return GCOO_EINVAL;
+        if (t.count > 0 && (!t.data || !t.out || !on_elements(t.data, t.type) || !on_elements(t.out, t.type))) return GCOO_EINVAL;
+        pieces += clip_pieces(t.count);
+        if (pieces > INT32_MAX) return GCOO_EINVAL;
+    }
+    return pieces;
+}
+
+// No `out` overlaps another tensor or its own data, but as data itself: the ranges in the order of their addresses, those that are written marked.
+int check_clip_ranges(const gcoo_gradient* list, int64_t tensors)
+{
+    struct Range { uintptr_t from, to; bool written; };
+    std::unique_ptr<Range[]> r(new (std::nothrow) Range[2 * (size_t)tensors + 1]);
+    if (!r) return GCOO_ENOMEM;
+    size_t n = 0;
+    for (int64_t i = 0; i < tensors; ++i) {
+        const gcoo_gradient& t = list[i];
+        if (t.count == 0) continue;
+        const uintptr_t bytes = (uintptr_t)t.count * gcoo::type_bytes(t.type), o = reinterpret_cast<uintptr_t>(t.out), d = reinterpret_cast<uintptr_t>(t.data);
+        if (o + bytes < o || d + bytes < d) return GCOO_EINVAL;
+        r[n++] = {o, o + bytes, true};
+        if (t.out != t.data) r[n++] = {d, d + bytes, false};
+    }
+    std::sort(r.get(), r.get() + n, [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t end_any = 0, end_written = 0;
+    for (size_t i = 0; i < n; ++i) {
+        if (r[i].from < end_written || (r[i].written && r[i].from < end_any)) return GCOO_EINVAL;
+        end_any = std::max(end_any, r[i].to);
+        if (r[i].written) end_written = std::max(end_written, r[i].to);
+    }
+    return GCOO_OK;
+}
+
+// f(list of a launch) for the tensors, as many as a launch takes at a time.
+template <typename F>
+int each_clip_launch(const gcoo_gradient* list, int64_t tensors, F&& f)
+{
+    gcoo::ClipList l{};
+    for (int64_t i = 0; i <= tensors; ++i) {
+        if (l.tensors > 0 && (i == tensors || l.tensors == gcoo::kClipTensors)) {
+            const int rc = f(l);
+            if (rc != GCOO_OK) return rc;
+            l.piece0 += l.pieces;
+            l.tensors = l.pieces = 0;
+        }
+        if (i < tensors && list[i].count > 0) {
+            l.t[l.tensors++] = {list[i].data, list[i].out, list[i].count, list[i].type, l.pieces};
+            l.pieces += (int32_t)clip_pieces(list[i].count);
+        }
+    }
+    return GCOO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gcoo_clip_grad_norm_bytes(const gcoo_gradient* list, int64_t tensors)
+{
+    const int64_t pieces = check_clip(list, tensors);
+    return pieces > 0 ? aligned((size_t)pieces * sizeof(double)) : 0;
+}
+
+int gcoo_clip_grad_norm(const gcoo_gradient* list, int64_t tensors, float max_norm, float* norm_dev, void* work, size_t work_bytes, void* stream)
+{
+    const int64_t pieces = check_clip(list, tensors);
+    if (pieces < 0) return (int)pieces;
+    if (!norm_dev || !on_floats(norm_dev) || !(max_norm >= 0.0f)) return GCOO_EINVAL;
+    int rc = check_clip_ranges(list, tensors);
+    if (rc == GCOO_OK) rc = check_work(work, work_bytes, gcoo_clip_grad_norm_bytes(list, tensors));
+    if (rc != GCOO_OK) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    double* sums = static_cast<double*>(work);
+    if (pieces == 0) return done(gcoo::launch_clip_scale(gcoo::ClipList{}, nullptr, 0, max_norm, norm_dev, s), "clip_scale launch");
+    rc = each_clip_launch(list, tensors, [&](const gcoo::ClipList& l) { return done(gcoo::launch_clip_sum(l, sums, s), "clip_sum launch"); });
+    if (rc != GCOO_OK) return rc;
+    return each_clip_launch(list, tensors, [&](const gcoo::ClipList& l) {
+        return done(gcoo::launch_clip_scale(l, sums, (int32_t)pieces, max_norm, l.piece0 == 0 ? norm_dev : nullptr, s), "clip_scale launch");
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,29 @@
+// Launch interface of the clipping of gradients (layer_clip.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gcoo {
+
+constexpr int kClipThreads = 256;
+constexpr int64_t kClipPiece = 65536;          // elements of a tensor that a workgroup takes
+constexpr int kClipTensors = 80;               // of one launch: their descriptions are its arguments
+
+struct ClipTensor {
+    const void* data;
+    void* out;
+    int64_t count;
+    int32_t type;
+    int32_t first;                             // its first piece among those of the launch
+};
+struct ClipList {
+    ClipTensor t[kClipTensors];                // none of them empty
+    int32_t tensors, pieces;
+    int64_t piece0;                            // pieces of the launches before
+};
+// sums[piece0 + i] = the squares of piece i
+hipError_t launch_clip_sum(const ClipList& l, double* sums, hipStream_t s);
+// scales the pieces by the norm that all `pieces_all` sums give; norm_out may be null
+hipError_t launch_clip_scale(const ClipList& l, const double* sums, int32_t pieces_all, float max_norm, float* norm_out, hipStream_t s);
+
+}  // namespace gcoo

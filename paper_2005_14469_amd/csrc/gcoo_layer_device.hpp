@@ -1,0 +1,64 @@
+// What the kernels of a sparse layer share: elements of the three types, activations and their slopes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gcoo.h"
+
+namespace gcoo {
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+template <typename T> __device__ __forceinline__ float widen(T x) { return (float)x; }
+template <typename T> __device__ __forceinline__ T narrow(float x) { return (T)x; }        // to nearest even
+
+// f(T) for the element type `type`.
+template <typename F>
+auto with_type(int type, F&& f)
+{
+    if (type == GCOO_BF16) return f(bf16_t{});
+    if (type == GCOO_F16) return f(f16_t{});
+    return f(float{});
+}
+
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
+constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f, kRootHalf = 0.7071067811865476f, kDensity0 = 0.3989422804014327f;
+
+__device__ __forceinline__ float activate(int act, float z)
+{
+    switch (act) {
+        case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : z;
+        case GCOO_ACT_SILU: return z * logistic(z);
+        case GCOO_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kRootHalf));
+        case GCOO_ACT_GELU_TANH: return z * logistic(2.0f * kGeluA * (z + kGeluB * z * z * z));
+        default: return z;
+    }
+}
+// (z s(q z + r z^3))' at z, s the logistic function: s + z s (1 - s) (q + 3 r z^2).  1 - s is E s, E = exp(-(q z + r z^3)): the difference would have lost what the factors behind it
+// need.  `c` is z held where E is finite; what is left out there is below 1e-18.
+__device__ __forceinline__ float slope_of_gate(float z, float c, float q, float r)
+{
+    const float c2 = c * c, e = __expf(-c * (q + r * c2)), s = __builtin_amdgcn_rcpf(1.0f + e);
+    return z != z ? z : s + c * s * (e * s) * (q + 3.0f * r * c2);
+}
+// dC act'(z)
+__device__ __forceinline__ float slope_times(int act, float z, float d)
+{
+    switch (act) {
+        case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : d;
+        case GCOO_ACT_SILU: return slope_of_gate(z, fminf(fmaxf(z, -80.0f), 80.0f), 1.0f, 0.0f) * d;
+        case GCOO_ACT_GELU: return d * (0.5f * (1.0f + erff(z * kRootHalf)) + z * kDensity0 * __expf(-0.5f * z * z));
+        case GCOO_ACT_GELU_TANH: return slope_of_gate(z, fminf(fmaxf(z, -8.0f), 8.0f), 2.0f * kGeluA, 2.0f * kGeluA * kGeluB) * d;
+        default: return d;
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+
+}  // namespace gcoo

@@ -1,0 +1,102 @@
+"""A layer with sparse weights in 64 bits on the CPU, from its formulas, and how far the kernels may be off.
+
+Rounding to a type is off by at most u = eps / 2 of the value (and half of the smallest number that float16 holds).  A sum of n products in fp32, in
+any order, is off by at most (n + 2) 2^-24 of the sum of the products' magnitudes.  The activations are z times a factor whose error is at most 2^-20: exp by a
+product and a power of two, (1.5 |x| + 2) 2^-24 of its value, a reciprocal of one unit in the last place, erf of at most 16; |x| times the slope of the logistic function is below
+0.23.  Their slopes are below 1.13, and off by at most 2^-19: two such factors and their sum."""
+import math
+
+import numpy as np
+import torch
+
+U = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+LEAST = {torch.float32: 0.0, torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
+SLOPE = 1.13
+F32 = 2.0 ** -24
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+
+
+def _logistic(x):
+    with np.errstate(over="ignore"):
+        return 1.0 / (1.0 + np.exp(-x))
+
+
+def activate(name, z):
+    if name == "relu":
+        return np.maximum(z, 0.0)
+    if name == "silu":
+        return z * _logistic(z)
+    if name == "gelu":
+        return 0.5 * z * (1.0 + _erf(z / math.sqrt(2.0)))
+    if name == "gelu_tanh":
+        return 0.5 * z * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (z + 0.044715 * z ** 3)))
+    return z
+
+
+def slope(name, z):
+    if name == "relu":
+        return (z > 0).astype(np.float64)
+    if name == "silu":
+        return _logistic(z) * (1.0 + z * _logistic(-z))
+    if name == "gelu":
+        return 0.5 * (1.0 + _erf(z / math.sqrt(2.0))) + z * np.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+    if name == "gelu_tanh":
+        a = math.sqrt(2.0 / math.pi)
+        t = np.tanh(a * (z + 0.044715 * z ** 3))
+        return 0.5 * (1.0 + t) + 0.5 * z * (1.0 - t * t) * a * (1.0 + 3 * 0.044715 * z * z)
+    return np.ones_like(z)
+
+
+def f64(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+def dense(m, k, row_ptr, cols, vals):
+    """The weights and their magnitudes as dense matrices (entries that repeat add up)."""
+    rows = np.repeat(np.arange(m), np.diff(row_ptr))
+    W, M = np.zeros((m, k)), np.zeros((m, k))
+    np.add.at(W, (rows, cols), vals.astype(np.float64))
+    np.add.at(M, (rows, cols), np.abs(vals.astype(np.float64)))
+    return W, M
+
+
+def forward(W, M, lens, B, bias, act, residual, dtype):
+    """((C, Z), how far each may be off); B, bias, residual as float64 arrays of what the kernel gets."""
+    z, d = W @ B, M @ np.abs(B)
+    off = (lens[:, None] + 2) * F32 * d
+    if bias is not None:
+        z = z + bias[:, None]
+        off = off + F32 * np.abs(z)
+    y = activate(act, z)
+    off_y = SLOPE * off + (0.0 if act in ("none", "relu") else 2.0 ** -20 * (np.abs(z) + off))
+    if residual is not None:
+        y = y + residual
+        off_y = off_y + F32 * np.abs(y)
+    u, least = U[dtype], LEAST[dtype]
+    return (y, z), (off_y + u * (np.abs(y) + off_y) + least, off + u * (np.abs(z) + off) + least)
+
+
+def epilogue_grad(dC, Z, act, dtype):
+    """((dZ, dbias), how far each may be off)"""
+    g = dC if act == "none" else dC * slope(act, Z)
+    off = np.zeros_like(g) if act in ("none", "relu") else 2.0 ** -19 * np.abs(dC)
+    u, least = U[dtype], LEAST[dtype]
+    n = dC.shape[1]
+    return (g, g.sum(1)), (off + u * (np.abs(g) + off) + least, (off + (n + 1) * F32 * (np.abs(g) + off)).sum(1))
+
+
+def grad_values(row_ptr, cols, dZ, B):
+    rows = np.repeat(np.arange(len(row_ptr) - 1), np.diff(row_ptr))
+    n = dZ.shape[1]
+    return (dZ[rows] * B[cols]).sum(1), (n + 2) * F32 * (np.abs(dZ[rows]) * np.abs(B[cols])).sum(1)
+
+
+def check(got, want, off, what=""):
+    got = f64(got)
+    assert got.shape == want.shape, what
+    finite = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    assert np.array_equal(got[~finite & ~np.isnan(want)], want[~finite & ~np.isnan(want)]), what
+    bad = np.abs(got[finite] - want[finite]) > off[finite]
+    assert not bad.any(), (what, int(bad.sum()), float((np.abs(got - want)[finite] / np.maximum(off[finite], 1e-300)).max()))
