@@ -50,16 +50,4 @@ struct EpilogueGradArgs {
 };
 hipError_t launch_epilogue_grad(const EpilogueGradArgs& a, hipStream_t s);
 
-struct GradValuesArgs {
-    RowsView A;
-    const void* dZ;
-    int64_t lddz;
-    const void* B;
-    int64_t ldb;
-    int64_t N;
-    int32_t type;
-    float* dvals;
-};
-hipError_t launch_grad_values(const GradValuesArgs& a, hipStream_t s);
-
 }  // namespace gcoo

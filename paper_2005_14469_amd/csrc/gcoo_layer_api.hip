@@ -1,6 +1,7 @@
 // Host side of the operators of a sparse layer (include/gcoo.h): argument checks, workspaces and launches.
 #include "gcoo_layer.hpp"
 #include "gcoo_layer_clip.hpp"
+#include "gcoo_layer_values.hpp"
 
 #include <algorithm>
 #include <memory>
@@ -120,14 +121,18 @@ int check_values(const gcoo::RowsView& A, const void* dZ, int64_t lddz, const vo
     return N > 0 && A.nnz > 0 && (!dZ || !B) ? GCOO_EINVAL : GCOO_OK;
 }
 
+size_t values_bytes(const gcoo::RowsView& A, const gcoo::ValuesPlan& p) { return p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0; }
+
 }  // namespace
 
 extern "C" {
 
 size_t gcoo_spdm_grad_values_bytes(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type)
 {
-    if (!A || check_values(gcoo::rows_view(A), dZ_dev, lddz, B_dev, ldb, N, type) != GCOO_OK) return 0;
-    return 0;
+    if (!A) return 0;
+    const gcoo::RowsView v = gcoo::rows_view(A);
+    if (check_values(v, dZ_dev, lddz, B_dev, ldb, N, type) != GCOO_OK || v.nnz == 0) return 0;
+    return values_bytes(v, gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb));
 }
 
 int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type,
@@ -139,10 +144,11 @@ int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz
     if (rc != GCOO_OK) return rc;
     if (!on_floats(dvals_dev) || (v.nnz > 0 && !dvals_dev)) return GCOO_EINVAL;
     if (v.nnz == 0) return GCOO_OK;
-    rc = check_work(work, work_bytes, 0);
+    const gcoo::ValuesPlan plan = gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb);
+    rc = check_work(work, work_bytes, values_bytes(v, plan));
     if (rc != GCOO_OK) return rc;
     const gcoo::GradValuesArgs a{v, dZ_dev, lddz, B_dev, ldb, N, type, dvals_dev};
-    return done(gcoo::launch_grad_values(a, static_cast<hipStream_t>(stream)), "layer_values launch");
+    return done(gcoo::launch_grad_values(a, plan, static_cast<float*>(work), static_cast<hipStream_t>(stream)), "gradient of the values");
 }
 
 }  // extern "C"

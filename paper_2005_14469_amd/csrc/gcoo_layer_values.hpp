@@ -1,0 +1,33 @@
+// Launch interface of the gradient of the stored weights (layer_values.hip).
+#pragma once
+#include "gcoo_layer.hpp"
+
+namespace gcoo {
+
+constexpr int kValuesThreads = 256;
+
+struct GradValuesArgs {
+    RowsView A;
+    const void* dZ;
+    int64_t lddz;
+    const void* B;
+    int64_t ldb;
+    int64_t N;
+    int32_t type;
+    float* dvals;
+};
+
+// How the gradients are computed: `parts` of N one by one, whose sums of all entries are joined afterwards.
+enum ValuesKernel { kValuesFew, kValuesEntries };
+struct ValuesPlan {
+    ValuesKernel kernel;
+    int32_t parts;
+    int32_t pieces;        // kValuesEntries: pieces of 16 bytes of a lane
+    bool one;              // a wave has one row of A, not four
+    bool any;              // B by addresses in 64 bits
+};
+ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb);
+// part: parts x nnz sums where there is more than one part
+hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, float* part, hipStream_t s);
+
+}  // namespace gcoo

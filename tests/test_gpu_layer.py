@@ -269,6 +269,29 @@ def test_grad_values_of_a_dense_matrix():
     assert torch.equal(binding.gcoo_spdm_grad_values(binding.gcoo_from_dense(W, 32), dZ[:, :0], B[:, :0]), torch.zeros(len(want), device=DEV))
 
 
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_far_apart(dtype):
+    """Offsets into B (and dZ) beyond 32 bits."""
+    T = TYPES[dtype]
+    pitch = 2 ** 30 - 8
+    for N in (1, 70, 300):
+        print(f"far apart: {dtype} N={N}", flush=True)
+        m, k = 9, 11
+        arrays = csr(m, k, 0.5, 3)
+        A = matrix(m, k, arrays)
+        far = torch.empty((k - 1) * pitch + N + 1, dtype=T, device=DEV)
+        rng = np.random.default_rng(N)
+        near, dZ = normal(rng, k, N, dtype=T), normal(rng, m, N, dtype=T)
+        for shift in (0, 1):
+            B = far[shift:].as_strided((k, N), (pitch, 1))
+            B.copy_(near)
+            assert torch.equal(binding.gcoo_spdm_grad_values(A, dZ, B), binding.gcoo_spdm_grad_values(A, dZ, near))
+            assert torch.equal(binding.gcoo_spdm_epilogue(A, B, activation="silu"), binding.gcoo_spdm_epilogue(A, near, activation="silu"))
+        Z = far.as_strided((m, N), (pitch, 1))
+        Z.copy_(dZ)
+        assert torch.equal(binding.gcoo_spdm_grad_values(A, Z, near), binding.gcoo_spdm_grad_values(A, dZ, near))
+
+
 # ---- clipping ----
 
 def clip_reference(tensors, max_norm):
