@@ -121,7 +121,8 @@ int check_values(const gcoo::RowsView& A, const void* dZ, int64_t lddz, const vo
     return N > 0 && A.nnz > 0 && (!dZ || !B) ? GCOO_EINVAL : GCOO_OK;
 }
 
-size_t values_bytes(const gcoo::RowsView& A, const gcoo::ValuesPlan& p) { return p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0; }
+// Where the tiles of a row begin, then the sums of the parts.
+size_t values_bytes(const gcoo::RowsView& A, const gcoo::ValuesPlan& p) { return aligned((size_t)p.starts * 4) + (p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0); }
 
 }  // namespace
 
@@ -148,7 +149,8 @@ int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz
     rc = check_work(work, work_bytes, values_bytes(v, plan));
     if (rc != GCOO_OK) return rc;
     const gcoo::GradValuesArgs a{v, dZ_dev, lddz, B_dev, ldb, N, type, dvals_dev};
-    return done(gcoo::launch_grad_values(a, plan, static_cast<float*>(work), static_cast<hipStream_t>(stream)), "gradient of the values");
+    float* part = reinterpret_cast<float*>(static_cast<char*>(work) + aligned((size_t)plan.starts * 4));
+    return done(gcoo::launch_grad_values(a, plan, static_cast<int32_t*>(work), part, static_cast<hipStream_t>(stream)), "gradient of the values");
 }
 
 }  // extern "C"

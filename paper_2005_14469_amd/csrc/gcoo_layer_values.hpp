@@ -18,16 +18,18 @@ struct GradValuesArgs {
 };
 
 // How the gradients are computed: `parts` of N one by one, whose sums of all entries are joined afterwards.
-enum ValuesKernel { kValuesFew, kValuesEntries };
+enum ValuesKernel { kValuesFew, kValuesEntries, kValuesTiles };
+constexpr int values_tile_cols(bool large) { return large ? 256 : 128; }
 struct ValuesPlan {
     ValuesKernel kernel;
     int32_t parts;
-    int32_t pieces;        // kValuesEntries: pieces of 16 bytes of a lane
+    int32_t pieces;        // kValuesEntries: pieces of 16 bytes of a lane; kValuesTiles: 4 for tiles of 256 x 256, 2 of 128 x 128
     bool one;              // a wave has one row of A, not four
     bool any;              // B by addresses in 64 bits
+    int64_t starts;        // kValuesTiles: words for where the tiles of a row begin
 };
 ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb);
-// part: parts x nnz sums where there is more than one part
-hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, float* part, hipStream_t s);
+// starts: plan.starts words; part: parts x nnz sums where there is more than one part
+hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, hipStream_t s);
 
 }  // namespace gcoo

@@ -2,7 +2,7 @@
 #include "gcoo_layer_values.hpp"
 #include "gcoo_layer_device.hpp"
 
-#include <type_traits>
+#include <atomic>
 
 namespace gcoo {
 
@@ -105,7 +105,7 @@ __device__ __forceinline__ void values_batch(uint32_t off, const Pieces<T, P>& p
 
 template <typename T, int P, bool PART, bool ANY>
 struct ValuesTile {
-    static constexpr int E = Piece<T>::kElements, AT_ONCE = P == 1 ? 16 : (P == 2 ? 8 : 4);
+    static constexpr int E = Piece<T>::kElements;
     const GradValuesArgs& a;
     float* out;
     Pieces<T, P> pc;
@@ -171,16 +171,23 @@ struct ValuesTile {
             const int32_t at = e;
             e += step;
             next = offset(e, end);
+            // as many of the sixteen as the fullest slot of the wave has: a load past a row's end returns at once, but holds the address path as long as any other
             float sums[16];
-            if constexpr (AT_ONCE == 16) values_batch<T, P, PART, ANY, 0, 16>(off, pc, B, z, sums);
-            else if constexpr (AT_ONCE == 8) {
-                values_batch<T, P, PART, ANY, 0, 8>(off, pc, B, z, sums);
-                values_batch<T, P, PART, ANY, 8, 8>(off, pc, B, z, sums);
+            const int32_t left = end - (at - (lane & 15));
+            if constexpr (P == 1) {
+                if (__any(left > 8)) values_batch<T, P, PART, ANY, 0, 16>(off, pc, B, z, sums);
+                else if (__any(left > 4)) values_batch<T, P, PART, ANY, 0, 8>(off, pc, B, z, sums);
+                else values_batch<T, P, PART, ANY, 0, 4>(off, pc, B, z, sums);
+            } else if constexpr (P == 2) {
+                if (__any(left > 4)) values_batch<T, P, PART, ANY, 0, 8>(off, pc, B, z, sums);
+                else values_batch<T, P, PART, ANY, 0, 4>(off, pc, B, z, sums);
+                if (__any(left > 12)) values_batch<T, P, PART, ANY, 8, 8>(off, pc, B, z, sums);
+                else if (__any(left > 8)) values_batch<T, P, PART, ANY, 8, 4>(off, pc, B, z, sums);
             } else {
                 values_batch<T, P, PART, ANY, 0, 4>(off, pc, B, z, sums);
-                values_batch<T, P, PART, ANY, 4, 4>(off, pc, B, z, sums);
-                values_batch<T, P, PART, ANY, 8, 4>(off, pc, B, z, sums);
-                values_batch<T, P, PART, ANY, 12, 4>(off, pc, B, z, sums);
+                if (__any(left > 4)) values_batch<T, P, PART, ANY, 4, 4>(off, pc, B, z, sums);
+                if (__any(left > 8)) values_batch<T, P, PART, ANY, 8, 4>(off, pc, B, z, sums);
+                if (__any(left > 12)) values_batch<T, P, PART, ANY, 12, 4>(off, pc, B, z, sums);
             }
             const float s = slot_sums(sums, lane);
             if (at < end) out[at] = s;
@@ -265,6 +272,201 @@ __global__ __launch_bounds__(kValuesThreads) void values_few(GradValuesArgs a)
     }
 }
 
+// ---- by matrix instructions: whole tiles of dZ x B^T, of which the entries are taken ----
+//
+// For matrices that are not very sparse every product of a row of dZ and a row of B is computed, by matrix instructions, in tiles of TM rows of A x TN columns, and the stored entries
+// are picked out of the tile's sums: 16-bit types reach sixteen times the rate of vector instructions so, and a row of B is fetched once per TM rows of A.  A tile without entries is not
+// computed.  Both operands lie along N, 128 bytes of each row (a step) at a time: from memory to registers while the step before is multiplied, to LDS, and from
+// there to the matrix instructions by 16 bytes per lane.  Where those bytes lie in a step is the same for both operands, so the instructions may take them in any order.
+// 16 bytes of row r are at piece ^ (r / 2 mod 8) of its 128 in LDS: sixteen lanes that read one piece of sixteen rows, and sixteen that write two rows, meet all 64 banks once.
+// For few tiles N is cut into parts, whose sums are joined afterwards.
+template <typename T> struct Mfma;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <> struct Mfma<bf16_t> {
+    static __device__ __forceinline__ void step(const u32x4& a, const u32x4& b, f32x16& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Piece<bf16_t>::vec, a), __builtin_bit_cast(Piece<bf16_t>::vec, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<f16_t> {
+    static __device__ __forceinline__ void step(const u32x4& a, const u32x4& b, f32x16& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Piece<f16_t>::vec, a), __builtin_bit_cast(Piece<f16_t>::vec, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<float> {
+    static __device__ __forceinline__ void step(const u32x4& a, const u32x4& b, f32x16& c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[i]), __uint_as_float(b[i]), c, 0, 0, 0);
+    }
+};
+
+// starts[r][t] = the first entry of row r whose column is in tile t or behind it, t = 0 .. tiles; starts[r][0] = -1 where the columns of the row do not ascend.  A wave per row.
+__global__ __launch_bounds__(kValuesThreads) void values_starts(RowsView A, int32_t tiles, int32_t tile_cols, int32_t* starts)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * (kValuesThreads / 64) + (threadIdx.x >> 6);
+    if (r >= A.m) return;
+    int32_t* to = starts + r * (tiles + 1);
+    const int32_t beg = A.start[r], end = A.start[r + 1];
+    const uint32_t kmax = (uint32_t)(A.k - 1);
+    auto tile_of = [&](int32_t e) {
+        const uint32_t c = (uint32_t)A.cols[e];
+        return (int32_t)((c < kmax ? c : kmax) / (uint32_t)tile_cols);
+    };
+    bool falls = false;
+    for (int32_t e0 = beg; e0 < end; e0 += 64) {
+        const int32_t e = e0 + lane;
+        if (e >= end) continue;
+        const int32_t t = tile_of(e), before = e > beg ? tile_of(e - 1) : 0;
+        falls |= before > t;
+        for (int32_t x = before + 1; x <= t; ++x) to[x] = e;
+        if (e == end - 1)
+            for (int32_t x = t + 1; x <= tiles; ++x) to[x] = end;
+    }
+    if (end <= beg)
+        for (int32_t x = 1 + lane; x <= tiles; x += 64) to[x] = beg;
+    const bool any = __any(falls);
+    if (lane == 0) to[0] = any ? -1 : beg;
+}
+
+// WM x WN waves, each MI x 2 tiles of 32 x 32.
+template <typename T, int WM, int WN, int MI>
+__global__ __launch_bounds__(64 * WM * WN, 2) void values_tiles(GradValuesArgs a, const int32_t* __restrict__ starts, float* out0, int32_t tiles_m, int32_t tiles_n, int32_t parts, int32_t part_steps)
+{
+    constexpr int TM = WM * MI * 32, TN = WN * 64, TH = 64 * WM * WN, E = Piece<T>::kElements, STEP = 8 * E, STAGE = (TM + TN) * 128, NA = TM * 8 / TH, NB = TN * 8 / TH;
+    static_assert(TM * 8 % TH == 0 && TN * 8 % TH == 0 && TM <= TH && TH % 16 == 0, "pieces and rows of a thread");
+    extern __shared__ __attribute__((aligned(16))) char smem[];               // two steps of both operands; then 64 rows of sums
+    __shared__ int32_t from[TM], to[TM];
+    const int t = (int)threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WN, wn = wave % WN;
+
+    // An XCD has a stretch of the tiles, in groups of four rows of tiles, column by column: few rows of both operands at a time.
+    const int32_t total = tiles_m * tiles_n * parts, per = (total + 7) / 8, item = (int32_t)(blockIdx.x & 7u) * per + (int32_t)(blockIdx.x >> 3);
+    if (item >= total || (int32_t)(blockIdx.x >> 3) >= per) return;           // the whole workgroup
+    const int32_t part = item / (tiles_m * tiles_n), at = item - part * (tiles_m * tiles_n), group = at / (4 * tiles_n), in = at - group * (4 * tiles_n);
+    const int32_t high = tiles_m - 4 * group < 4 ? tiles_m - 4 * group : 4, tn = in / high, tm = 4 * group + in - tn * high;
+    const int64_t m = a.A.m, k = a.A.k, N = a.N, r0 = (int64_t)tm * TM, c0 = (int64_t)tn * TN;
+
+    // the entries of the tile, row by row
+    int some = 0;
+    if (t < TM) {
+        int32_t f = 0, e = 0;
+        if (r0 + t < m) {
+            const int32_t* s = starts + (r0 + t) * (tiles_n + 1);
+            if (s[0] < 0) { f = a.A.start[r0 + t]; e = a.A.start[r0 + t + 1]; }
+            else { f = tn == 0 ? s[0] : s[tn]; e = s[tn + 1]; }
+        }
+        from[t] = f;
+        to[t] = e;
+        some = f < e;
+    }
+    if (!__syncthreads_or(some)) return;
+
+    // this thread's pieces of a step: piece t % 8 of rows t / 8 + i TH / 8
+    const char *pa[NA], *pb[NB];
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+        const int64_t r = r0 + t / 8 + i * (TH / 8);
+        pa[i] = reinterpret_cast<const char*>(static_cast<const T*>(a.dZ) + (r < m ? r : m - 1) * a.lddz + (t & 7) * E);
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int64_t c = c0 + t / 8 + i * (TH / 8);
+        pb[i] = reinterpret_cast<const char*>(static_cast<const T*>(a.B) + (c < k ? c : k - 1) * a.ldb + (t & 7) * E);
+    }
+    const int64_t steps_all = (N + STEP - 1) / STEP, s0 = (int64_t)part * part_steps, s1 = s0 + part_steps < steps_all ? s0 + part_steps : steps_all;
+    u32x4 va[NA], vb[NB];
+    auto fetch = [&](int64_t s) {
+        const int64_t n = N - s * STEP;
+        if (n >= STEP) {
+#pragma unroll
+            for (int i = 0; i < NA; ++i) __builtin_memcpy(&va[i], pa[i] + s * 128, 16);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) __builtin_memcpy(&vb[i], pb[i] + s * 128, 16);
+        } else {
+            // the last step: what is behind column N is 0 in both operands
+            const int own = (int)n - (t & 7) * E;
+            auto piece = [&](const char* p) {
+                typename Piece<T>::vec x;
+#pragma unroll
+                for (int u = 0; u < E; ++u) x[u] = u < own ? reinterpret_cast<const T*>(p + s * 128)[u] : (T)0.0f;
+                return __builtin_bit_cast(u32x4, x);
+            };
+#pragma unroll
+            for (int i = 0; i < NA; ++i) va[i] = piece(pa[i]);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) vb[i] = piece(pb[i]);
+        }
+    };
+    // (TH / 8 is a multiple of 16 or 32: the swizzle of a thread's rows is the same for all of them)
+    const int put_at = t / 8 * 128 + (((t & 7) ^ (t >> 4 & 7)) * 16);
+    auto put = [&](char* stage) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) *reinterpret_cast<u32x4*>(stage + put_at + i * (TH / 8) * 128) = va[i];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) *reinterpret_cast<u32x4*>(stage + TM * 128 + put_at + i * (TH / 8) * 128) = vb[i];
+    };
+
+    f32x16 acc[MI][2];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = 0.0f;
+    const int l32 = lane & 31, half = lane >> 5, swizzle = l32 >> 1 & 7;
+    const char *ga = smem + (wm * MI * 32 + l32) * 128, *gb = smem + (TM + wn * 64 + l32) * 128;
+    fetch(s0);
+    put(smem);
+    __syncthreads();
+    for (int64_t s = s0; s < s1; ++s) {
+        const int stage = (int)((s - s0) & 1) * STAGE;
+        if (s + 1 < s1) fetch(s + 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int piece = stage + (((2 * q + half) ^ swizzle) * 16);
+            u32x4 fa[MI], fb[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) fb[j] = *reinterpret_cast<const u32x4*>(gb + j * 32 * 128 + piece);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const u32x4*>(ga + i * 32 * 128 + piece);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) Mfma<T>::step(fa[i], fb[j], acc[i][j]);
+        }
+        if (s + 1 < s1) put(smem + (STAGE - stage));
+        __syncthreads();
+    }
+
+    // 64 rows of sums at a time through LDS; TH / 64 threads take the entries of a row
+    float* sums = reinterpret_cast<float*>(smem);
+    float* out = out0 + (int64_t)part * a.A.nnz;
+    const uint32_t kmax = (uint32_t)(k - 1);
+    constexpr int LANES = TH / 64;
+#pragma unroll
+    for (int q = 0; q < TM / 64; ++q) {
+        if (wm == q / (MI / 2)) {
+            constexpr int PER = MI / 2;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        sums[(i * 32 + 8 * (x / 4) + 4 * half + x % 4) * TN + wn * 64 + j * 32 + l32] = acc[(q % PER) * 2 + i][j][x];
+        }
+        __syncthreads();
+        const int r = t / LANES;
+        const int32_t end = to[q * 64 + r];
+#pragma unroll 4
+        for (int32_t e = from[q * 64 + r] + t % LANES; e < end; e += LANES) {
+            const uint32_t c = (uint32_t)a.A.cols[e], col = (c < kmax ? c : kmax) - (uint32_t)c0;
+            if (col < (uint32_t)TN) out[e] = sums[r * TN + (int)col];
+        }
+        __syncthreads();
+    }
+}
+
 // ---- dvals[e] = the sums of the tiles or parts, in their order ----
 __global__ __launch_bounds__(kValuesThreads) void values_join(const float* __restrict__ part, float* __restrict__ dvals, int64_t nnz, int32_t parts)
 {
@@ -303,26 +505,79 @@ static hipError_t launch_few(const GradValuesArgs& a, hipStream_t s)
     return hipGetLastError();
 }
 
+template <typename T, int WM, int WN, int MI>
+static hipError_t launch_tiles(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, hipStream_t s)
+{
+    constexpr int TM = WM * MI * 32, TN = WN * 64, lds = 2 * (TM + TN) * 128;
+    static_assert(64 * TN * 4 <= lds && TN == values_tile_cols(MI == 4), "the sums of 64 rows");
+    const auto kernel = &values_tiles<T, WM, WN, MI>;
+    // more LDS than the default limit of a workgroup: asked for once per device
+    static std::atomic<unsigned> done[64];
+    int dev = -1;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+    if (!done[dev].load(std::memory_order_acquire)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+        done[dev].store(1u, std::memory_order_release);
+    }
+    const int64_t tiles_m = (a.A.m + TM - 1) / TM, tiles_n = (a.A.k + TN - 1) / TN, total = tiles_m * tiles_n * plan.parts;
+    if (total > 0x7ffffff0LL) return hipErrorInvalidConfiguration;
+    const int64_t steps = (a.N * (int64_t)sizeof(T) + 127) / 128;
+    values_starts<<<dim3((unsigned)((a.A.m + kValuesThreads / 64 - 1) / (kValuesThreads / 64))), dim3(kValuesThreads), 0, s>>>(a.A, (int32_t)tiles_n, TN, starts);
+    kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WM * WN), lds, s>>>(a, starts, plan.parts > 1 ? part : a.dvals, (int32_t)tiles_m, (int32_t)tiles_n, plan.parts,
+                                                                                   (int32_t)((steps + plan.parts - 1) / plan.parts));
+    return hipGetLastError();
+}
+
+// Times of the two kernels, in microseconds, of which the shorter is taken.  Entries: what they take of B through the vector caches, both matrices from memory once.  Tiles: all products of
+// m x k x N, then the entries one by one.  Against 126 products (256 to 8000 rows and columns, N = 64 to 8000, 0.5 to 20 % stored, bf16 and fp32) the one so chosen takes 1.5 % longer than the faster of
+// the two on average (bf16, us, entries and tiles: 8000 x 8000, N = 8000, 1 %: 545 977, 5 %: 2226 1011; 4000 x 4000, N = 4000, 2 %: 131 147, 5 %: 296 148; 2000 x 2000, N = 512, 5 %: 16 20, 10 %: 24 21;
+// fp32: 8000 x 8000, N = 8000, 5 %: 4411 8088, 20 %: 16597 8141; 2000 x 2000, N = 4000, 10 %: 246 272).
+static double entries_time(double nnz, double rows, double bytes, bool odd16) { return 5.0 + nnz * bytes / (odd16 ? 12.5e6 : 22e6) + rows * bytes / 5e6; }
+static double tiles_time(double m, double k, double nnz, double N, int type)
+{
+    return (type == GCOO_F32 ? 15.0 : 12.0) + 2.0 * m * k * N / (type == GCOO_F32 ? 0.122e9 : 0.9e9) + nnz * 5e-6;
+}
+
 ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb)
 {
-    (void)nnz;
     const int64_t size = (int64_t)type_bytes(type), bytes = N * size;
-    ValuesPlan p{kValuesFew, 1, 1, false, false};
+    ValuesPlan p{kValuesFew, 1, 1, false, false, 0};
     if (bytes <= 64) return p;
-    p.kernel = kValuesEntries;
+    // (buffer loads at multiples of 4 bytes only)
     p.any = (uint64_t)k * (uint64_t)ldb * (uint64_t)size > kRowsMaxBytes || reinterpret_cast<uintptr_t>(B) % 4 != 0 || ldb * size % 4 != 0 || bytes % 4 != 0;
-    p.one = m < 2048;
+    if (tiles_time((double)m, (double)k, (double)nnz, (double)N, type) < entries_time((double)nnz, (double)(m + k), (double)bytes, p.any && size == 2)) {
+        // tiles of 256 x 256 where they fill the compute units, else of 128 x 128 and as many parts of N as fill them twice, of four steps and more
+        p.kernel = kValuesTiles;
+        p.pieces = type != GCOO_F32 && ((m + 255) / 256) * ((k + 255) / 256) >= 160 ? 4 : 2;
+        const int64_t edge = values_tile_cols(p.pieces == 4), tiles_n = (k + edge - 1) / edge, tiles = ((m + edge - 1) / edge) * tiles_n, steps = (bytes + 127) / 128;
+        const int64_t wanted = p.pieces == 4 ? 1 : (512 + tiles - 1) / tiles, most = (steps + 3) / 4, parts = wanted < most ? wanted : most, each = (steps + parts - 1) / parts;
+        p.parts = (int32_t)((steps + each - 1) / each);                    // none of them empty
+        p.starts = m * (tiles_n + 1);
+        return p;
+    }
+    // The widest tile of B of which an XCD's L2 keeps all rows (us, 1, 2 and 4 pieces: bf16, 0.5 %: 2000 x 2000, N = 4000: 24.6 22.6 22.1; 4000 x 4000, N = 4000: 53.0 48.6 47.4; 8000 x 8000, N = 8000:
+    // 319 297 379; 14000 x 14000, N = 2000: 287 342 398; fp32: 4000 x 4000, N = 4000: 82 70 76; 8000 x 8000, N = 8000: 581 563 778), and one tile where N allows it.
+    p.kernel = kValuesEntries;
     if (bytes <= 1024) p.pieces = bytes <= 256 ? 1 : (bytes <= 512 ? 2 : 4);
-    else p.pieces = k <= 3000 ? 4 : (k <= 6000 ? 2 : 1);
+    else p.pieces = k <= 3500 ? 4 : (k <= 10000 ? 2 : 1);
     p.parts = (int32_t)((bytes + 256 * p.pieces - 1) / (256 * p.pieces));
+    p.one = m * p.parts < 4096 && nnz >= 12 * m;
     return p;
 }
 
-hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, float* part, hipStream_t s)
+hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, hipStream_t s)
 {
-    if (plan.kernel == kValuesFew) return with_type(a.type, [&](auto t) { return launch_few<decltype(t)>(a, s); });
     hipError_t e = with_type(a.type, [&](auto t) {
         typedef decltype(t) T;
+        if (plan.kernel == kValuesFew) return launch_few<T>(a, s);
+        if (plan.kernel == kValuesTiles) {
+            if constexpr (sizeof(T) == 2)
+                if (plan.pieces == 4) return launch_tiles<T, 2, 4, 4>(a, plan, starts, part, s);
+            return launch_tiles<T, 2, 2, 2>(a, plan, starts, part, s);
+        }
         return plan.pieces == 1 ? launch_entries<T, 1>(a, plan, part, s) : (plan.pieces == 2 ? launch_entries<T, 2>(a, plan, part, s) : launch_entries<T, 4>(a, plan, part, s));
     });
     if (e != hipSuccess || plan.parts == 1) return e;
