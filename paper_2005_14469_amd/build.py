@@ -51,7 +51,7 @@ def _checked(src: str) -> bool:
     """Sources whose generated code is verified by isa_check (kernels that issue loads from asm, that load straight to LDS next
     to the index mode, or whose workgroups hand words to each other without release and acquire)."""
     name = os.path.basename(src)
-    return name.startswith("spdm_sched_v") or name in ("spdm_share.hip", "spdm_band.hip", "gcoo_api.hip")
+    return name.startswith(("spdm_sched_v", "layer_band_")) or name in ("spdm_share.hip", "spdm_band.hip", "gcoo_api.hip")
 
 
 def _compile(src: str) -> str:
@@ -90,6 +90,9 @@ def verify_generated_code() -> None:
         if stem == "spdm_band":
             verify_band_code(stem, text)
             continue
+        if stem.startswith("layer_band_"):
+            verify_band_code(stem, text, "layer_bandI" + {"f32": "f", "bf16": "DF16b", "f16": "DF16_"}[stem.rsplit("_", 1)[1]])
+            continue
         if stem == "gcoo_api":
             verify_count_code(stem, text)
             continue
@@ -119,20 +122,22 @@ def verify_share_code(stem: str, text: str) -> None:
         raise RuntimeError(f"{stem}: register spills {spills}")
 
 
-def verify_band_code(stem: str, text: str) -> None:
-    """The sixteen-wave kernel, its instances (four and two columns per lane): no register spills, 128 VGPRs at most (four waves per SIMD), every load
+def verify_band_code(stem: str, text: str, name: str = "spdm_bandI") -> None:
+    """The sixteen-wave kernel (and with the epilogue of a layer: its instances for a type), its instances (four and two columns per lane): no register spills, 128 VGPRs at most (four waves per SIMD), every load
     that writes LDS sets M0 itself, nothing is in flight at a barrier, and its asm text writes the scalar registers that its clobber list names."""
     from . import isa_check
     instances = [(4, 0, 0), (4, 0, 1), (4, 1, 0), (4, 1, 1), (2, 0, 0), (2, 0, 1), (2, 1, 0)]
     for v, spread, late in instances:
-        kernel = f"_ZN4gcoo9spdm_bandILi{v}ELb{spread}ELb{late}E"
+        kernel = f"_ZN4gcoo{len(name) - len(name.partition('I')[2]) - 1}{name}Li{v}ELb{spread}ELb{late}E"
         loads, problems = isa_check.check_lds_loads(text, kernel, asm_only=True)
         if loads < 15 or problems or isa_check.check_lds_loads(text, kernel)[0] != loads:
             raise RuntimeError(f"{stem} {kernel}: {loads} loads to LDS, {problems[:3]}")
         written, read = isa_check.asm_scalar_writes(text, kernel)
         if written != set(range(12, 32)) | set(range(36, 100)) | ({100} if v == 2 else set()) or not read:
             raise RuntimeError(f"{stem} {kernel}: scalar registers written {sorted(written)}, read {sorted(read)}")
-    meta = text[text.index("amdhsa.kernels"):]
+    # (beside them there is one for uneven rows, of ordinary code)
+    kernels = text[text.index("amdhsa.kernels"):].split("  - .agpr_count")[1:]
+    meta = "".join(x for x in kernels if "layer_rows_all" not in x)
     for key, most in (("vgpr_spill_count", 0), ("sgpr_spill_count", 0), ("private_segment_fixed_size", 0), ("vgpr_count", 128)):
         got = [int(x) for x in re.findall(rf"\.{key}:\s+(\d+)", meta)]
         if len(got) != len(instances) or max(got) > most:

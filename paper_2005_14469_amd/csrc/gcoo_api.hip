@@ -1623,6 +1623,25 @@ int kernel_of_product(const gcoo_matrix** M, const Shape& sh, const float* B_dev
     return A->has_sched ? GCOO_KERNEL_SCHED : GCOO_KERNEL_ROWS;
 }
 
+gcoo::RowsArgs rows_args(const gcoo_matrix* A, const float* B, int64_t ldb, int64_t N, float* C, int64_t ldc)
+{
+    gcoo::RowsArgs rows{A->row_start(), A->row_cols(), A->row_vals(), A->m, A->k, A->nnz, B, ldb, N, C, ldc,
+                        A->long_rows(), A->long_count(), gcoo::rows_long(A->m, A->nnz), long_room(A->m, A->nnz), 0};
+    if (A->long_places) {
+        // no places are looked at where only a row that repeats columns could be long
+        const bool some = A->k > rows.long_row;
+        rows.long_count = nullptr;
+        rows.long_room = some ? (int32_t)(A->nnz / rows.long_row) : 0;
+        if (!some) rows.long_row = INT32_MAX;
+    }
+    return rows;
+}
+gcoo::BandArgs band_args(const gcoo_matrix* A, const float* B, int64_t ldb, int64_t N, float* C, int64_t ldc)
+{
+    return {A->band_head(), A->band_units(), A->band_first(), A->band_count(), (int32_t)gcoo::band_blocks(A->m, A->L.band.h), A->L.band.h, A->L.band.v,
+            0, 0, A->uneven(), gcoo::band_head_stride(A->k, A->L.band.v), A->m, A->k, B, ldb, N, C, ldc};
+}
+
 }  // namespace
 
 extern "C" {
@@ -1655,24 +1674,14 @@ int gcoo_spdm_variant(const gcoo_matrix* A, const float* B_dev, int64_t ldb, int
         return GCOO_OK;
     }
     if (kernel == GCOO_KERNEL_ROWS || kernel == GCOO_KERNEL_BAND) {
-        gcoo::RowsArgs rows{A->row_start(), A->row_cols(), A->row_vals(), A->m, A->k, A->nnz, B_dev, ldb, N, C_dev, ldc,
-                            A->long_rows(), A->long_count(), gcoo::rows_long(A->m, A->nnz), long_room(A->m, A->nnz), 0};
-        if (A->long_places) {
-            // no places are looked at where only a row that repeats columns could be long
-            const bool some = A->k > rows.long_row;
-            rows.long_count = nullptr;
-            rows.long_room = some ? (int32_t)(A->nnz / rows.long_row) : 0;
-            if (!some) rows.long_row = INT32_MAX;
-        }
+        const gcoo::RowsArgs rows = rows_args(A, B_dev, ldb, N, C_dev, ldc);
         if (kernel == GCOO_KERNEL_ROWS) {
             const bool lines = ldb % 32 == 0 && reinterpret_cast<uintptr_t>(B_dev) % 128 == 0, reach = (uint64_t)A->k * (uint64_t)ldb * 4u <= gcoo::kRowsMaxBytes;
             const TilePlan& plan = tile_plan(A->m, A->k, A->nnz, N);
             hipError_t e = reach && plan.preferred[lines] ? gcoo::launch_spdm_rows_tile(rows, plan.row_wgs, plan.whole, s) : gcoo::launch_spdm_rows(rows, !A->from_csr, s);
             return e == hipSuccess ? GCOO_OK : hip_fail(e, "spdm_rows launch");
         }
-        gcoo::BandArgs a{A->band_head(), A->band_units(), A->band_first(), A->band_count(), (int32_t)gcoo::band_blocks(A->m, A->L.band.h), A->L.band.h, A->L.band.v,
-                         0, 0, A->uneven(), gcoo::band_head_stride(A->k, A->L.band.v), A->m, A->k, B_dev, ldb, N, C_dev, ldc};
-        hipError_t e = gcoo::launch_spdm_band(a, rows, s);
+        hipError_t e = gcoo::launch_spdm_band(band_args(A, B_dev, ldb, N, C_dev, ldc), rows, s);
         return e == hipSuccess ? GCOO_OK : hip_fail(e, "spdm_band launch");
     }
     if (kernel == GCOO_KERNEL_SHARE) {
@@ -1789,5 +1798,59 @@ RowsView rows_view(const gcoo_matrix* A)
     return {A->m, A->k, A->nnz, A->row_start(), A->row_cols(), A->row_vals()};
 }
 int hip_failed(hipError_t e, const char* what) { return hip_fail(e, what); }
+
+// The times are those of the products in fp32.  Row by row a B of 2-byte elements is one of half as many columns, and twice that where it has to be read by 64-bit addresses; the bands are of fp32, which costs a pass over B.
+ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64_t N, int type)
+{
+    if (A->inner) A = A->inner;
+    const int64_t m = A->m, k = A->k, nnz = A->nnz, size = (int64_t)type_bytes(type);
+    if (nnz == 0 || k < 1) return {kProductNone, 0, 0};
+    if (N < 16 / size) return {kProductRows, 0, 0};
+    const int64_t N4 = size == 4 ? N : (N + 1) / 2;
+    const bool lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0;
+    const double slow = odd_elements(B, ldb, N, type) ? 2.0 : 1.0;
+    ProductPlan p{kProductRows, 0, 0};
+    double best = slow * rows_time(m, k, nnz, N4, lines);
+    const TilePlan& tile = tile_plan(m, k, nnz, N);
+    if (tile.row_wgs > 0 && tile.time < 0.85 * slow * few_columns_rows_time(m, k, nnz, N4, lines)) {
+        p.kernel = kProductTile;
+        best = std::min(best, tile.time + 1.0);
+    }
+    const BandPlan band = A->L.band;
+    if (band.h > 0) {
+        const int64_t ldw = size == 4 ? ldb : (N + 31) / 32 * 32;
+        const bool aligned = N % 4 == 0 && ldw % 4 == 0 && (size == 2 || reinterpret_cast<uintptr_t>(B) % 16 == 0);
+        const double t = band_time(m, k, nnz, N, band, size == 2 || lines) + (size == 2 ? 2.0 + 6.0 * (double)k * (double)N / 4.5e6 : 0.0);
+        if ((aligned || N >= 64 * band.v) && (uint64_t)k * (uint64_t)ldw * 4u <= kRowsMaxBytes && t < best) {
+            p.kernel = kProductBand;
+            if (size == 2) { p.ldw = ldw; p.work = al((size_t)k * (size_t)ldw * 4); }
+        }
+    }
+    return p;
+}
+
+hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const void* B, int64_t ldb, int64_t N, const EpilogueArgs& e, void* work, hipStream_t s)
+{
+    if (A->inner) A = A->inner;
+    if (plan.kernel == kProductNone) return launch_epilogue(A->m, N, e, s);
+    const float* wide = static_cast<const float*>(B);
+    if (plan.work > 0) {
+        float* to = static_cast<float*>(work);
+        const hipError_t err = launch_widen(B, ldb, e.type, to, plan.ldw, A->k, N, s);
+        if (err != hipSuccess) return err;
+        wide = to;
+        ldb = plan.ldw;
+    }
+    const RowsArgs rows = rows_args(A, wide, ldb, N, nullptr, N);
+    if (plan.kernel == kProductTile) {
+        const TilePlan& tile = tile_plan(A->m, A->k, A->nnz, N);
+        return launch_layer_tile(rows, e, tile.row_wgs, tile.whole, s);
+    }
+    if (plan.kernel == kProductBand) {
+        const BandArgs band = band_args(A, wide, ldb, N, nullptr, N);
+        return e.type == GCOO_F32 ? launch_layer_band_f32(band, rows, e, s) : (e.type == GCOO_BF16 ? launch_layer_band_bf16(band, rows, e, s) : launch_layer_band_f16(band, rows, e, s));
+    }
+    return e.type == GCOO_F32 ? launch_layer_rows_f32(rows, e, s) : (e.type == GCOO_BF16 ? launch_layer_rows_bf16(rows, e, s) : launch_layer_rows_f16(rows, e, s));
+}
 
 }  // namespace gcoo

@@ -39,18 +39,6 @@ int check_product(const gcoo::RowsView& A, const void* B, int64_t ldb, int64_t N
     return GCOO_OK;
 }
 
-// B in fp32 where it is not, and the product in front of the epilogue.
-struct ProductPlan { size_t wide_b, product, total; int64_t ldw; };
-ProductPlan product_plan(const gcoo::RowsView& A, int64_t N, int type)
-{
-    ProductPlan p{0, 0, 0, (N + 31) / 32 * 32};
-    if (A.nnz == 0 || A.m == 0 || N == 0) return p;
-    if (type != GCOO_F32) { p.wide_b = 0; p.total += aligned((size_t)A.k * (size_t)p.ldw * 4); }
-    p.product = p.total;
-    p.total += aligned((size_t)A.m * (size_t)p.ldw * 4);
-    return p;
-}
-
 }  // namespace
 
 extern "C" {
@@ -59,7 +47,7 @@ size_t gcoo_spdm_epilogue_bytes(const gcoo_matrix* A, const void* B_dev, int64_t
 {
     if (!A) return 0;
     const gcoo::RowsView v = gcoo::rows_view(A);
-    return check_product(v, B_dev, ldb, N, e, C_dev, ldc) == GCOO_OK ? product_plan(v, N, e->type).total : 0;
+    return check_product(v, B_dev, ldb, N, e, C_dev, ldc) == GCOO_OK && N > 0 && v.m > 0 ? gcoo::product_plan(A, B_dev, ldb, N, e->type).work : 0;
 }
 
 int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int64_t N, const gcoo_epilogue* e, void* C_dev, int64_t ldc,
@@ -69,23 +57,11 @@ int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int
     const gcoo::RowsView v = gcoo::rows_view(A);
     int rc = check_product(v, B_dev, ldb, N, e, C_dev, ldc);
     if (rc != GCOO_OK || N == 0 || v.m == 0) return rc;
-    const ProductPlan plan = product_plan(v, N, e->type);
-    rc = check_work(work, work_bytes, plan.total);
+    const gcoo::ProductPlan plan = gcoo::product_plan(A, B_dev, ldb, N, e->type);
+    rc = check_work(work, work_bytes, plan.work);
     if (rc != GCOO_OK) return rc;
-    hipStream_t s = static_cast<hipStream_t>(stream);
     const gcoo::EpilogueArgs args{e->bias, e->residual, e->ldr, e->Z, e->ldz, C_dev, ldc, e->type, e->activation};
-    if (v.nnz == 0) return done(gcoo::launch_epilogue(nullptr, 0, v.m, N, args, s), "layer_epilogue launch");
-    float* P = reinterpret_cast<float*>(static_cast<char*>(work) + plan.product);
-    const float* B = static_cast<const float*>(B_dev);
-    if (e->type != GCOO_F32) {
-        float* W = reinterpret_cast<float*>(static_cast<char*>(work) + plan.wide_b);
-        rc = done(gcoo::launch_widen(B_dev, ldb, e->type, W, plan.ldw, v.k, N, s), "layer_widen launch");
-        if (rc != GCOO_OK) return rc;
-        B = W;
-        ldb = plan.ldw;
-    }
-    rc = gcoo_spdm(A, B, ldb, N, P, plan.ldw, stream);
-    return rc != GCOO_OK ? rc : done(gcoo::launch_epilogue(P, plan.ldw, v.m, N, args, s), "layer_epilogue launch");
+    return done(gcoo::launch_product(A, plan, B_dev, ldb, N, args, work, static_cast<hipStream_t>(stream)), "product with its epilogue");
 }
 
 size_t gcoo_epilogue_grad_bytes(int64_t m, int64_t N)

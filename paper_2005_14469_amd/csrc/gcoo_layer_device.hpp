@@ -35,6 +35,18 @@ __device__ __forceinline__ float activate(int act, float z)
         default: return z;
     }
 }
+// the same for N values: one look at `act` for all of them
+template <int N>
+__device__ __forceinline__ void activate_all(int act, float (&z)[N])
+{
+    if (act == GCOO_ACT_NONE) return;
+#define GCOO_EACH(A) _Pragma("unroll") for (int u = 0; u < N; ++u) z[u] = activate(A, z[u]);
+    if (act == GCOO_ACT_RELU) { GCOO_EACH(GCOO_ACT_RELU) }
+    else if (act == GCOO_ACT_SILU) { GCOO_EACH(GCOO_ACT_SILU) }
+    else if (act == GCOO_ACT_GELU) { GCOO_EACH(GCOO_ACT_GELU) }
+    else { GCOO_EACH(GCOO_ACT_GELU_TANH) }
+#undef GCOO_EACH
+}
 // (z s(q z + r z^3))' at z, s the logistic function: s + z s (1 - s) (q + 3 r z^2).  1 - s is E s, E = exp(-(q z + r z^3)): the difference would have lost what the factors behind it
 // need.  `c` is z held where E is finite; what is left out there is below 1e-18.
 __device__ __forceinline__ float slope_of_gate(float z, float c, float q, float r)

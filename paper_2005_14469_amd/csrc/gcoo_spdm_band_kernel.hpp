@@ -314,13 +314,63 @@ struct BandRowsGrid { int32_t tiles, rpw, wave_row; };
 // A matrix with a list of far more entries than the others (take_rows and band_mark say so on the device, where the
 // row lengths are) has no schedule: the waves would wait for that list in every band.  Its rows are multiplied one by one, by the
 // workgroups of this launch.
-template <int V, bool SPREAD, bool LATE>            // V = 4: the wide cut, 2: the tall one; when the rows of the next band are requested
-__global__ __launch_bounds__(64 * kBandWaves) void spdm_band(BandArgs a, RowsArgs by_rows, BandRowsGrid rg)
+// What becomes of the sums of a (block, tile): here they are C.  `lane_at`, `fillw`: the lane's columns in a row of B in LDS, the wave's rows inside a band buffer.  The operators of a sparse layer have
+// another (layer_band.hpp).
+struct BandPlain {
+    typedef RowsPlain Rows;
+    static constexpr bool kRowsToo = true;          // uneven rows are multiplied one by one in the same launch
+    template <int V>
+    static __device__ __forceinline__ void store(const BandAcc& acc, uint32_t lane_at, uint32_t fillw);
+};
+template <int V>
+__device__ __forceinline__ void BandPlain::store(const BandAcc& acc, uint32_t lane_at, uint32_t fillw)
+{
+    constexpr int32_t kTile = BandCut<V>::kTile;
+    // What the stores need is made again from the kernel's arguments: the loop leaves the compiler no vector register and eighteen
+    // scalar ones, too few to carry it across.
+    typedef const __attribute__((address_space(4))) char* arg_ptr;
+    arg_ptr args = (arg_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    uint32_t bid = blockIdx.x;
+    asm volatile("" : "+s"(args), "+s"(bid));
+    const __attribute__((address_space(4))) BandArgs* z = (const __attribute__((address_space(4))) BandArgs*)args;
+    const int32_t item2 = (int32_t)(bid & 7u) * (int32_t)(z->grid >> 3) + (int32_t)(bid >> 3);
+    const int32_t tile2 = item2 / z->blocks, Q2 = item2 - tile2 * z->blocks;
+    const int32_t N = (int32_t)z->N, first = tile2 * kTile, base = first > N - kTile && N >= kTile ? N - kTile : first;
+    const int32_t jc = base + (int32_t)(lane_at >> 2);             // the lane's first column; it stores those from `first` on
+    if (jc + V > first && jc < N) {
+        const int own = first > jc ? first - jc : 0;
+        const int32_t h = z->h;
+        const int64_t row0 = ((int64_t)Q2 * kBandWaves + fillw / (uint32_t)kBandFillBytes) * h, ldc = z->ldc;
+        const int64_t rows = z->m - row0 < h ? z->m - row0 : h;
+        float* __restrict__ dst = z->C + jc + row0 * ldc;
+        constexpr int kStride = BandCut<V>::kMaxH + 1;
+        typedef float vec __attribute__((ext_vector_type(V), aligned(4)));         // rows of C are aligned to 4 bytes only
+#pragma unroll
+        for (int r = 0; r < BandCut<V>::kMaxH; ++r) {
+            if (r < rows) {
+                vec o;
+#pragma unroll
+                for (int v = 0; v < V; ++v) o[v] = band_acc_get(acc, v * kStride + r);
+                if (own == 0) {
+                    __builtin_nontemporal_store(o, reinterpret_cast<vec*>(dst));
+                } else {
+#pragma unroll
+                    for (int v = 1; v < V; ++v)
+                        if (v >= own) __builtin_nontemporal_store(o[v], dst + v);
+                }
+            }
+            dst += ldc;
+        }
+    }
+}
+
+template <int V, bool SPREAD, bool LATE, class OUT>            // V = 4: the wide cut, 2: the tall one; when the rows of the next band are requested
+__device__ __forceinline__ void band_item(const BandArgs& a, const RowsArgs& by_rows, const BandRowsGrid& rg, const typename OUT::Rows& rows_io)
 {
     static_assert(V == 4 || !(SPREAD && LATE), "");
     extern __shared__ __attribute__((aligned(16))) uint32_t band_smem[];
     if (*a.uneven != 0u) {
-        rows_all<16>(by_rows, rg.tiles, rg.rpw, rg.wave_row, *reinterpret_cast<RowsAllLds*>(band_smem));
+        if constexpr (OUT::kRowsToo) rows_all<16>(by_rows, rows_io, rg.tiles, rg.rpw, rg.wave_row, *reinterpret_cast<RowsAllLds*>(band_smem));
         return;
     }
     // XCD-aware order: XCD x walks the contiguous slice [x*per, (x+1)*per) of the tile-major list, so the blocks that run on
@@ -491,42 +541,13 @@ __global__ __launch_bounds__(64 * kBandWaves) void spdm_band(BandArgs a, RowsArg
 #undef BD_WAIT_BAND
     }
 
-    // What the stores need is made again from the kernel's arguments: the loop leaves the compiler no vector register and eighteen
-    // scalar ones, too few to carry it across.
-    typedef const __attribute__((address_space(4))) char* arg_ptr;
-    arg_ptr args = (arg_ptr)__builtin_amdgcn_kernarg_segment_ptr();
-    uint32_t bid = blockIdx.x;
-    asm volatile("" : "+s"(args), "+s"(bid));
-    const __attribute__((address_space(4))) BandArgs* z = (const __attribute__((address_space(4))) BandArgs*)args;
-    const int32_t item2 = (int32_t)(bid & 7u) * (int32_t)(z->grid >> 3) + (int32_t)(bid >> 3);
-    const int32_t tile2 = item2 / z->blocks, Q2 = item2 - tile2 * z->blocks;
-    const int32_t N = (int32_t)z->N, first = tile2 * kTile, base = first > N - kTile && N >= kTile ? N - kTile : first;
-    const int32_t jc = base + (int32_t)(lane_at >> 2);             // the lane's first column; it stores those from `first` on
-    if (jc + V > first && jc < N) {
-        const int own = first > jc ? first - jc : 0;
-        const int32_t h = z->h;
-        const int64_t row0 = ((int64_t)Q2 * kBandWaves + fillw / (uint32_t)kBandFillBytes) * h, ldc = z->ldc;
-        const int64_t rows = z->m - row0 < h ? z->m - row0 : h;
-        float* __restrict__ dst = z->C + jc + row0 * ldc;
-        constexpr int kStride = BandCut<V>::kMaxH + 1;
-        typedef float vec __attribute__((ext_vector_type(V), aligned(4)));         // rows of C are aligned to 4 bytes only
-#pragma unroll
-        for (int r = 0; r < BandCut<V>::kMaxH; ++r) {
-            if (r < rows) {
-                vec o;
-#pragma unroll
-                for (int v = 0; v < V; ++v) o[v] = band_acc_get(acc, v * kStride + r);
-                if (own == 0) {
-                    __builtin_nontemporal_store(o, reinterpret_cast<vec*>(dst));
-                } else {
-#pragma unroll
-                    for (int v = 1; v < V; ++v)
-                        if (v >= own) __builtin_nontemporal_store(o[v], dst + v);
-                }
-            }
-            dst += ldc;
-        }
-    }
+    OUT::template store<V>(acc, lane_at, fillw);
+}
+
+template <int V, bool SPREAD, bool LATE>
+__global__ __launch_bounds__(64 * kBandWaves) void spdm_band(BandArgs a, RowsArgs by_rows, BandRowsGrid rg)
+{
+    band_item<V, SPREAD, LATE, BandPlain>(a, by_rows, rg, RowsPlain{});
 }
 
 }  // namespace gcoo

@@ -115,6 +115,12 @@ inline int32_t rows_moved(int64_t m, int64_t nnz, int64_t N, const float* C, int
     if (ldc % 32 == 0 && reinterpret_cast<uintptr_t>(C) % 128 == 0) return 0;
     return nnz <= 4 * m || (nnz <= 8 * m && m * N >= 25000000) || (N > 128 && N <= 160) ? 31 : 0;
 }
+// How the row-by-row kernel cuts a product: lanes to a row (of 16 bytes of B each), sums that a lane keeps.  For B of 2-byte elements it is asked with half of N and ldb: rows of as many bytes.
+struct RowsWidth { int lanes, sums; };
+RowsWidth rows_width(const RowsArgs& a);
+// Its launch with tiles of `tile` columns by `lanes` lanes to a row.
+struct RowsGrid { int64_t tiles, row_wgs, rpw, grid; int32_t wave_row; };
+RowsGrid rows_grid(const RowsArgs& a, int lanes, int64_t tile, int64_t N4);
 // Largest B (k x ldb) whose rows a buffer descriptor reaches with something left above for the entries past the end of a row.
 constexpr uint64_t kRowsMaxBytes = 0xffffefffull;
 // `spread`: long rows in places are taken by rows_turn().

@@ -25,6 +25,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "gcoo_spdm_launch.hpp"
 
 namespace gcoo {
@@ -112,9 +114,35 @@ __device__ __forceinline__ void tile_entries(__amdgpu_buffer_rsrc_t cols, __amdg
     }
 }
 
+// B and C as they are here: pieces of four fp32 columns, and the sums.  The operators of a sparse layer have others (layer_tile.hip).
+struct TilePlain {
+    __amdgpu_buffer_rsrc_t B;
+    uint32_t ldb4;
+    __device__ __forceinline__ TilePlain(const RowsArgs& a, int32_t jb)
+    {
+        B = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.B + jb), 0, (int)(uint32_t)((uint64_t)(a.k - 1) * (uint64_t)a.ldb * 4u + kTileRowBytes), 0x00027000);
+        ldb4 = (uint32_t)a.ldb * 4u;
+    }
+    __device__ __forceinline__ tile_u32x4 piece(int32_t row, int32_t q) const { return __builtin_amdgcn_raw_buffer_load_b128(B, (int)((uint32_t)row * ldb4 + (uint32_t)q * 16u), 0, 0); }
+    // the sums of columns jc .. jc + 3 of row r, of which those from j0 on are the lane's
+    __device__ __forceinline__ void store(const RowsArgs& a, int64_t r, int32_t jc, int32_t j0, float (&acc)[4]) const
+    {
+        float* dst = a.C + r * a.ldc + jc;
+        if (jc >= j0) {
+            *reinterpret_cast<tile_f32x4_any*>(dst) = tile_f32x4{acc[0], acc[1], acc[2], acc[3]};
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (jc + u >= j0) dst[u] = acc[u];
+        }
+    }
+};
+
 // LDS: tile_lds_rows(), the bins where the tile comes to be.  Workgroup: (tile, rows [wg * rows, ...)), an XCD takes a stretch of them with the tiles side by side, so that the workgroups that read a
 // line of B do so through one L2.  `long_steps`: a row of more steps of four entries than this has a wave to itself.
-__global__ __launch_bounds__(kTileThreads, 8) void spdm_rows_tile(RowsArgs a, int32_t row_wgs, int32_t rows, int32_t total, int32_t long_steps)
+// make_io(first column): what the workgroup reads of B and does with the sums.
+template <class MakeIO>
+__device__ __forceinline__ void tile_item(const RowsArgs& a, int32_t row_wgs, int32_t rows, int32_t total, int32_t long_steps, MakeIO&& make_io)
 {
     extern __shared__ __attribute__((aligned(16))) char tile_smem[];
     __shared__ int32_t counts[2];                                  // long rows, items taken
@@ -132,14 +160,13 @@ __global__ __launch_bounds__(kTileThreads, 8) void spdm_rows_tile(RowsArgs a, in
 
     int32_t start = t <= mine ? a.row_ptr[r0 + t] : 0;
     // this workgroup's columns of B, on their way while its rows are put in order
-    __amdgpu_buffer_rsrc_t B = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.B + jb), 0, (int)(uint32_t)((uint64_t)(a.k - 1) * (uint64_t)a.ldb * 4u + kTileRowBytes), 0x00027000);
-    const uint32_t ldb4 = (uint32_t)a.ldb * 4u;
+    const auto io = make_io(jb);
     tile_u32x4 piece[kTileLoads];
 #pragma unroll
     for (int j = 0; j < kTileLoads; ++j) {
         const int32_t i = j * kTileThreads + t;
         if (j * kTileThreads < pieces)
-            piece[j] = i < pieces ? __builtin_amdgcn_raw_buffer_load_b128(B, (int)((uint32_t)(i / kTileLanes) * ldb4 + (uint32_t)(i % kTileLanes) * 16u), 0, 0) : 0u;
+            piece[j] = i < pieces ? io.piece(i / kTileLanes, i % kTileLanes) : 0u;
     }
     {
         const int32_t most = (int32_t)a.nnz;
@@ -222,18 +249,33 @@ __global__ __launch_bounds__(kTileThreads, 8) void spdm_rows_tile(RowsArgs a, in
                 for (int u = 0; u < 4; ++u) acc[u] += __shfl_xor(acc[u], d, 64);
         }
         if (now.row >= 0 && (x >= n_long || slot == 0)) {
-            float* dst = a.C + (r0 + now.row) * a.ldc + jc;
-            if (jc >= j0) {
-                *reinterpret_cast<tile_f32x4_any*>(dst) = tile_f32x4{acc[0], acc[1], acc[2], acc[3]};
-            } else {
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (jc + u >= j0) dst[u] = acc[u];
-            }
+            io.store(a, r0 + now.row, jc, j0, acc);
         }
         x = x2;
         now = then;
     }
 }
+
+// Its launch; false where it does not serve the product.
+struct TileGrid { int64_t rows, wgs, total, lds; int32_t long_steps; };
+bool tile_grid(const RowsArgs& a, int64_t row_wgs, bool whole, TileGrid* g);
+
+// More LDS than the default limit of a workgroup: asked for once per device and kernel.
+struct TileLimit {
+    std::atomic<unsigned> done[64] = {};
+    hipError_t raise(const void* kernel)
+    {
+        int dev = -1;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+        if (!done[dev].load(std::memory_order_acquire)) {
+            e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kTileLdsBytes);
+            if (e != hipSuccess) return e;
+            done[dev].store(1u, std::memory_order_release);
+        }
+        return hipSuccess;
+    }
+};
 
 }  // namespace gcoo

@@ -1,51 +1,61 @@
 // Elementwise passes of a sparse layer, and their launchers.
 #include "gcoo_layer.hpp"
-#include "gcoo_layer_device.hpp"
+#include "gcoo_layer_io.hpp"
 
 namespace gcoo {
 
 constexpr int kPassThreads = 256;
 
-// A thread per element, rows by blockIdx.y.
+// A thread per eight elements, rows by blockIdx.y.
 template <typename T>
 __global__ __launch_bounds__(kPassThreads) void layer_widen(const T* __restrict__ src, int64_t lds, float* __restrict__ dst, int64_t ldd, int64_t rows, int64_t N)
 {
-    const int64_t j = (int64_t)blockIdx.x * kPassThreads + threadIdx.x;
+    const int64_t j = ((int64_t)blockIdx.x * kPassThreads + threadIdx.x) * 8;
     if (j >= N) return;
-    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) dst[r * ldd + j] = widen(src[r * lds + j]);
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        float x[8];
+        if (j + 8 <= N) layer_load<T, 8>(src, r * lds + j, x);
+        else
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = j + u < N ? widen(src[r * lds + j + u]) : 0.0f;
+        // (what lies behind N in the last piece is part of the padding of a row)
+        rows_f32x4* to = reinterpret_cast<rows_f32x4*>(dst + r * ldd + j);
+        to[0] = rows_f32x4{x[0], x[1], x[2], x[3]};
+        to[1] = rows_f32x4{x[4], x[5], x[6], x[7]};
+    }
 }
 
+// A matrix without entries.
 template <typename T>
-__global__ __launch_bounds__(kPassThreads) void layer_epilogue(const float* P, int64_t ldp, int64_t m, int64_t N, EpilogueArgs e)
+__global__ __launch_bounds__(kPassThreads) void layer_no_entries(int64_t m, int64_t N, EpilogueArgs e)
 {
     const int64_t j = (int64_t)blockIdx.x * kPassThreads + threadIdx.x;
     if (j >= N) return;
     for (int64_t r = blockIdx.y; r < m; r += gridDim.y) {
-        const float z = (P ? P[r * ldp + j] : 0.0f) + (e.bias ? e.bias[r] : 0.0f);
-        if (e.Z) static_cast<T*>(e.Z)[r * e.ldz + j] = narrow<T>(z);
-        float y = activate(e.activation, z);
-        if (e.residual) y += widen(static_cast<const T*>(e.residual)[r * e.ldr + j]);
-        static_cast<T*>(e.C)[r * e.ldc + j] = narrow<T>(y);
+        float x[1] = {0.0f}, res[1];
+        layer_residual<T, 1>(e, r, j, 0, 1, true, res);
+        layer_finish<T, 1>(e, r, j, 0, 1, x, res);
     }
 }
 
-static dim3 pass_grid(int64_t rows, int64_t N) { return dim3((unsigned)((N + kPassThreads - 1) / kPassThreads), (unsigned)(rows < 65535 ? rows : 65535)); }
+static dim3 pass_grid(int64_t rows, int64_t pieces) { return dim3((unsigned)((pieces + kPassThreads - 1) / kPassThreads), (unsigned)(rows < 65535 ? rows : 65535)); }
 
 hipError_t launch_widen(const void* src, int64_t lds, int type, float* dst, int64_t ldd, int64_t rows, int64_t N, hipStream_t s)
 {
-    if (rows < 1 || N < 1) return hipSuccess;
     return with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        layer_widen<T><<<pass_grid(rows, N), dim3(kPassThreads), 0, s>>>(static_cast<const T*>(src), lds, dst, ldd, rows, N);
-        return hipGetLastError();
+        if constexpr (sizeof(T) == 4) return hipErrorInvalidValue;
+        else {
+            layer_widen<T><<<pass_grid(rows, (N + 7) / 8), dim3(kPassThreads), 0, s>>>(static_cast<const T*>(src), lds, dst, ldd, rows, N);
+            return hipGetLastError();
+        }
     });
 }
 
-hipError_t launch_epilogue(const float* P, int64_t ldp, int64_t m, int64_t N, const EpilogueArgs& e, hipStream_t s)
+hipError_t launch_epilogue(int64_t m, int64_t N, const EpilogueArgs& e, hipStream_t s)
 {
-    if (m < 1 || N < 1) return hipSuccess;
     return with_type(e.type, [&](auto t) {
-        layer_epilogue<decltype(t)><<<pass_grid(m, N), dim3(kPassThreads), 0, s>>>(P, ldp, m, N, e);
+        layer_no_entries<decltype(t)><<<pass_grid(m, N), dim3(kPassThreads), 0, s>>>(m, N, e);
         return hipGetLastError();
     });
 }

@@ -1,0 +1,6 @@
+// The row-by-row product with its epilogue, f32.
+#include "gcoo_layer_rows.hpp"
+
+namespace gcoo {
+hipError_t launch_layer_rows_f32(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s) { return launch_layer_rows_of<float>(a, e, s); }
+}  // namespace gcoo

@@ -155,25 +155,25 @@ struct ValuesTile {
             for (int u = 0; u < E; ++u) z[q * E + u] = widen((T)x[u]);
         }
     }
-    __device__ __forceinline__ uint32_t offset(int32_t e, int32_t end) const
+    __device__ __forceinline__ uint32_t offset(uint32_t e, uint32_t end) const
     {
         if (e >= end) return kNowhere;
         const uint32_t c = (uint32_t)a.A.cols[e], in = c < kmax ? c : kmax;
         return ANY ? in : in * pitch;
     }
-    // The entries beg, beg + step, ... below end by sixteens, for each slot its own (every lane of the wave calls it); `shift`: of the slot inside a step.
-    __device__ __forceinline__ void entries(int32_t beg, int32_t end, int32_t step, const float (&z)[P * E]) const
+    // The entries beg, beg + step, ... below end by sixteens, for each slot its own (every lane of the wave calls it).  (Unsigned: a step beyond the last of 2^31 entries stays a number.)
+    __device__ __forceinline__ void entries(uint32_t beg, uint32_t end, uint32_t step, const float (&z)[P * E]) const
     {
-        int32_t e = beg + (lane & 15);
+        uint32_t e = beg + (uint32_t)(lane & 15);
         uint32_t next = offset(e, end);
-        while (__any(e - (lane & 15) < end)) {
+        while (__any(e - (uint32_t)(lane & 15) < end)) {
             const uint32_t off = next;
-            const int32_t at = e;
+            const uint32_t at = e;
             e += step;
             next = offset(e, end);
             // as many of the sixteen as the fullest slot of the wave has: a load past a row's end returns at once, but holds the address path as long as any other
             float sums[16];
-            const int32_t left = end - (at - (lane & 15));
+            const int32_t left = (int32_t)(end - (at - (uint32_t)(lane & 15)));
             if constexpr (P == 1) {
                 if (__any(left > 8)) values_batch<T, P, PART, ANY, 0, 16>(off, pc, B, z, sums);
                 else if (__any(left > 4)) values_batch<T, P, PART, ANY, 0, 8>(off, pc, B, z, sums);
@@ -260,8 +260,8 @@ __global__ __launch_bounds__(kValuesThreads) void values_few(GradValuesArgs a)
 #pragma unroll
     for (int j = 0; j < MOST; ++j) z[j] = j < N ? widen(src[j]) : 0.0f;
     const uint32_t kmax = (uint32_t)(a.A.k - 1);
-    const int32_t end = a.A.start[r + 1];
-    for (int32_t e = a.A.start[r] + (int32_t)(threadIdx.x & 15); e < end; e += 16) {
+    const uint32_t end = (uint32_t)a.A.start[r + 1];
+    for (uint32_t e = (uint32_t)a.A.start[r] + (threadIdx.x & 15); e < end; e += 16) {
         const uint32_t c = (uint32_t)a.A.cols[e];
         const T* b = static_cast<const T*>(a.B) + (int64_t)(c < kmax ? c : kmax) * a.ldb;
         float s = 0.0f;
@@ -316,9 +316,9 @@ __global__ __launch_bounds__(kValuesThreads) void values_starts(RowsView A, int3
         return (int32_t)((c < kmax ? c : kmax) / (uint32_t)tile_cols);
     };
     bool falls = false;
-    for (int32_t e0 = beg; e0 < end; e0 += 64) {
-        const int32_t e = e0 + lane;
-        if (e >= end) continue;
+    for (int64_t e0 = beg; e0 < end; e0 += 64) {
+        if (e0 + lane >= end) continue;
+        const int32_t e = (int32_t)e0 + lane;
         const int32_t t = tile_of(e), before = e > beg ? tile_of(e - 1) : 0;
         falls |= before > t;
         for (int32_t x = before + 1; x <= t; ++x) to[x] = e;
@@ -457,9 +457,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void values_tiles(GradValuesArgs a
         }
         __syncthreads();
         const int r = t / LANES;
-        const int32_t end = to[q * 64 + r];
+        const uint32_t end = (uint32_t)to[q * 64 + r];
 #pragma unroll 4
-        for (int32_t e = from[q * 64 + r] + t % LANES; e < end; e += LANES) {
+        for (uint32_t e = (uint32_t)(from[q * 64 + r] + t % LANES); e < end; e += LANES) {
             const uint32_t c = (uint32_t)a.A.cols[e], col = (c < kmax ? c : kmax) - (uint32_t)c0;
             if (col < (uint32_t)TN) out[e] = sums[r * TN + (int)col];
         }

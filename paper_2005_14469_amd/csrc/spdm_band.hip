@@ -1,29 +1,9 @@
 // The sixteen-wave SpDM kernel that reads the band schedule, and its launcher.
-#include "gcoo_spdm_band_kernel.hpp"
-
-#include <atomic>
+#include "gcoo_spdm_band_launch.hpp"
 
 namespace gcoo {
 
-template <int V, bool SPREAD, bool LATE>
-static hipError_t launch_band(const BandArgs& a, const RowsArgs& rows, const BandRowsGrid& rg, hipStream_t s)
-{
-    // more LDS than the default limit of a workgroup: asked for once per device
-    static std::atomic<unsigned> done[64];
-    int dev = -1;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
-    if (!done[dev].load(std::memory_order_acquire)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(&spdm_band<V, SPREAD, LATE>), hipFuncAttributeMaxDynamicSharedMemorySize, kBandLdsBytes);
-        if (e != hipSuccess) return e;
-        done[dev].store(1u, std::memory_order_release);
-    }
-    spdm_band<V, SPREAD, LATE><<<dim3((unsigned)(a.grid > kRowsAllWgs ? a.grid : kRowsAllWgs)), dim3(64 * kBandWaves), kBandLdsBytes, s>>>(a, rows, rg);
-    return hipGetLastError();
-}
-
-hipError_t launch_spdm_band(const BandArgs& a, const RowsArgs& rows, hipStream_t s)
+hipError_t band_launch(const BandArgs& a, const RowsArgs& rows, BandLaunch* out)
 {
     if (a.v != 2 && a.v != 4) return hipErrorInvalidValue;
     const int64_t tile = 64 * a.v, tiles = (a.N + tile - 1) / tile, total = a.blocks * tiles;
@@ -33,13 +13,15 @@ hipError_t launch_spdm_band(const BandArgs& a, const RowsArgs& rows, hipStream_t
     const bool aligned = a.N % 4 == 0 && a.ldb % 4 == 0 && reinterpret_cast<uintptr_t>(a.B) % 16 == 0;
     if (a.v == 2 && a.k > kBandTallMaxK) return hipErrorInvalidValue;
     if (!aligned && a.N < tile) return hipErrorInvalidValue;
-    BandArgs b = a;
+    BandArgs& b = out->a;
+    b = a;
     b.total = (int32_t)total;
     b.grid = (int32_t)((total + 7) / 8 * 8);                 // whole rounds over the 8 XCDs
-    BandRowsGrid rg;
+    BandRowsGrid& rg = out->grid;
     const int64_t mean = rows.nnz / rows.m, wave_row = 2 * mean > 64 ? 2 * mean : 64;
     if (rows.N < 4) return hipErrorInvalidConfiguration;
-    RowsArgs by_rows = rows;
+    RowsArgs& by_rows = out->rows;
+    by_rows = rows;
     by_rows.moved = rows_moved(rows.m, rows.nnz, rows.N, rows.C, rows.ldc);
     rg.tiles = (int32_t)((rows.N + by_rows.moved + 63) / 64);
     rg.rpw = 4;                                              // (8: as fast)
@@ -55,12 +37,29 @@ hipError_t launch_spdm_band(const BandArgs& a, const RowsArgs& rows, hipStream_t
     //   behind the second step      1.004    1.006    1.009    1.010    1.014    1.027    1.033    1.033    1.031     1.024
     //   behind the second unit      0.996    0.994    1.006    1.018    1.022    1.019    1.009    0.996    0.986     0.973
     const double entries = band_entries(a.m, a.k, rows.nnz, a.h, a.v);
-    if (a.v == 2) {
-        if (entries < 20.0) return launch_band<2, true, false>(b, by_rows, rg, s);
-        return entries < 37.0 ? launch_band<2, false, false>(b, by_rows, rg, s) : launch_band<2, false, true>(b, by_rows, rg, s);
+    if (a.v == 2) out->kind = entries < 20.0 ? kBandTallSpread : (entries < 37.0 ? kBandTallFirst : kBandTallSecond);
+    else out->kind = entries < 14.0 ? kBandWideSpread : (entries < 20.0 ? kBandWideStep : (entries < 42.0 ? kBandWideFirst : kBandWideSecond));
+    return hipSuccess;
+}
+
+struct PlainBand {
+    BandLaunch l;
+    template <int V, bool SPREAD, bool LATE>
+    hipError_t launch(hipStream_t s) const
+    {
+        static BandLimits limits;
+        const hipError_t e = limits.raise(reinterpret_cast<const void*>(&spdm_band<V, SPREAD, LATE>), l.kind);
+        if (e != hipSuccess) return e;
+        spdm_band<V, SPREAD, LATE><<<l.blocks(), dim3(64 * kBandWaves), kBandLdsBytes, s>>>(l.a, l.rows, l.grid);
+        return hipGetLastError();
     }
-    if (entries < 20.0) return entries < 14.0 ? launch_band<4, true, false>(b, by_rows, rg, s) : launch_band<4, true, true>(b, by_rows, rg, s);
-    return entries < 42.0 ? launch_band<4, false, false>(b, by_rows, rg, s) : launch_band<4, false, true>(b, by_rows, rg, s);
+};
+
+hipError_t launch_spdm_band(const BandArgs& a, const RowsArgs& rows, hipStream_t s)
+{
+    PlainBand b;
+    const hipError_t e = band_launch(a, rows, &b.l);
+    return e == hipSuccess ? launch_band_kind(b, s) : e;
 }
 
 }  // namespace gcoo
