@@ -67,6 +67,8 @@ struct EpilogueGradArgs {
     int64_t m, N;
     int32_t type, activation;
 };
-hipError_t launch_epilogue_grad(const EpilogueGradArgs& a, hipStream_t s);
+// Parts of a row; part: that many times m sums where there is more than one.
+int32_t epilogue_grad_parts(int64_t m, int64_t N);
+hipError_t launch_epilogue_grad(const EpilogueGradArgs& a, float* part, hipStream_t s);
 
 }  // namespace gcoo

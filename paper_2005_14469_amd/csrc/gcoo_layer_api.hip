@@ -66,8 +66,9 @@ int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int
 
 size_t gcoo_epilogue_grad_bytes(int64_t m, int64_t N)
 {
-    (void)m; (void)N;
-    return 0;
+    if (m < 0 || N < 0 || m > INT32_MAX || N > INT32_MAX) return 0;
+    const int32_t parts = gcoo::epilogue_grad_parts(m, N);
+    return parts > 1 ? aligned((size_t)parts * (size_t)m * 4) : 0;
 }
 
 int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const void* Z_dev, int64_t ldz, const void* dC_dev, int64_t lddc,
@@ -83,7 +84,7 @@ int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const voi
     const int rc = check_work(work, work_bytes, gcoo_epilogue_grad_bytes(m, N));
     if (rc != GCOO_OK || (!dbias_dev && (!dZ_dev || N == 0))) return rc;
     const gcoo::EpilogueGradArgs a{Z_dev, ldz, dC_dev, lddc, dZ_dev, lddz, dbias_dev, m, N, type, activation};
-    return done(gcoo::launch_epilogue_grad(a, static_cast<hipStream_t>(stream)), "layer_epilogue_grad launch");
+    return done(gcoo::launch_epilogue_grad(a, static_cast<float*>(work), static_cast<hipStream_t>(stream)), "layer_epilogue_grad launch");
 }
 
 }  // extern "C"
@@ -152,13 +153,15 @@ int64_t check_clip(const gcoo_gradient* list, int64_t tensors)
     return pieces;
 }
 
-// No `out` overlaps another tensor or its own data, but as data itself: the ranges in the order of their addresses, those that are written marked.
-int check_clip_ranges(const gcoo_gradient* list, int64_t tensors)
+// No `out`, and not the norm, overlaps another tensor or its own data, but as data itself: the ranges in the order of their addresses, those that are written marked.
+int check_clip_ranges(const gcoo_gradient* list, int64_t tensors, const float* norm)
 {
     struct Range { uintptr_t from, to; bool written; };
     std::unique_ptr<Range[]> r(new (std::nothrow) Range[2 * (size_t)tensors + 1]);
     if (!r) return GCOO_ENOMEM;
-    size_t n = 0;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
+    r[0] = {at, at + 4, true};
+    size_t n = 1;
     for (int64_t i = 0; i < tensors; ++i) {
         const gcoo_gradient& t = list[i];
         if (t.count == 0) continue;
@@ -177,16 +180,26 @@ int check_clip_ranges(const gcoo_gradient* list, int64_t tensors)
     return GCOO_OK;
 }
 
+// How many launches the tensors are, and how many workgroups each has at the most.
+struct ClipLaunches { int64_t launches, wgs; };
+ClipLaunches clip_launches(const gcoo_gradient* list, int64_t tensors)
+{
+    int64_t full = 0;
+    for (int64_t i = 0; i < tensors; ++i) full += list[i].count > 0;
+    const int64_t launches = (full + gcoo::kClipTensors - 1) / gcoo::kClipTensors;
+    return {launches, launches > 0 ? std::max<int64_t>(gcoo::kClipSums / launches, 64) : 0};
+}
 // f(list of a launch) for the tensors, as many as a launch takes at a time.
 template <typename F>
-int each_clip_launch(const gcoo_gradient* list, int64_t tensors, F&& f)
+int each_clip_launch(const gcoo_gradient* list, int64_t tensors, int64_t most_wgs, F&& f)
 {
     gcoo::ClipList l{};
     for (int64_t i = 0; i <= tensors; ++i) {
         if (l.tensors > 0 && (i == tensors || l.tensors == gcoo::kClipTensors)) {
+            l.wgs = (int32_t)std::min<int64_t>(l.pieces, most_wgs);
             const int rc = f(l);
             if (rc != GCOO_OK) return rc;
-            l.piece0 += l.pieces;
+            l.sum0 += l.wgs;
             l.tensors = l.pieces = 0;
         }
         if (i < tensors && list[i].count > 0) {
@@ -196,15 +209,15 @@ int each_clip_launch(const gcoo_gradient* list, int64_t tensors, F&& f)
     }
     return GCOO_OK;
 }
-
 }  // namespace
 
 extern "C" {
 
 size_t gcoo_clip_grad_norm_bytes(const gcoo_gradient* list, int64_t tensors)
 {
-    const int64_t pieces = check_clip(list, tensors);
-    return pieces > 0 ? aligned((size_t)pieces * sizeof(double)) : 0;
+    if (check_clip(list, tensors) <= 0) return 0;
+    const ClipLaunches n = clip_launches(list, tensors);
+    return aligned((size_t)(n.launches * n.wgs) * sizeof(double));
 }
 
 int gcoo_clip_grad_norm(const gcoo_gradient* list, int64_t tensors, float max_norm, float* norm_dev, void* work, size_t work_bytes, void* stream)
@@ -212,16 +225,21 @@ int gcoo_clip_grad_norm(const gcoo_gradient* list, int64_t tensors, float max_no
     const int64_t pieces = check_clip(list, tensors);
     if (pieces < 0) return (int)pieces;
     if (!norm_dev || !on_floats(norm_dev) || !(max_norm >= 0.0f)) return GCOO_EINVAL;
-    int rc = check_clip_ranges(list, tensors);
+    int rc = check_clip_ranges(list, tensors, norm_dev);
     if (rc == GCOO_OK) rc = check_work(work, work_bytes, gcoo_clip_grad_norm_bytes(list, tensors));
     if (rc != GCOO_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     double* sums = static_cast<double*>(work);
     if (pieces == 0) return done(gcoo::launch_clip_scale(gcoo::ClipList{}, nullptr, 0, max_norm, norm_dev, s), "clip_scale launch");
-    rc = each_clip_launch(list, tensors, [&](const gcoo::ClipList& l) { return done(gcoo::launch_clip_sum(l, sums, s), "clip_sum launch"); });
+    const int64_t most = clip_launches(list, tensors).wgs;
+    int32_t sums_all = 0;
+    rc = each_clip_launch(list, tensors, most, [&](const gcoo::ClipList& l) {
+        sums_all = l.sum0 + l.wgs;
+        return done(gcoo::launch_clip_sum(l, sums, s), "clip_sum launch");
+    });
     if (rc != GCOO_OK) return rc;
-    return each_clip_launch(list, tensors, [&](const gcoo::ClipList& l) {
-        return done(gcoo::launch_clip_scale(l, sums, (int32_t)pieces, max_norm, l.piece0 == 0 ? norm_dev : nullptr, s), "clip_scale launch");
+    return each_clip_launch(list, tensors, most, [&](const gcoo::ClipList& l) {
+        return done(gcoo::launch_clip_scale(l, sums, sums_all, max_norm, l.sum0 == 0 ? norm_dev : nullptr, s), "clip_scale launch");
     });
 }
 

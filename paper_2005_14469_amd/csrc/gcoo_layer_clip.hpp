@@ -6,8 +6,9 @@
 namespace gcoo {
 
 constexpr int kClipThreads = 256;
-constexpr int64_t kClipPiece = 65536;          // elements of a tensor that a workgroup takes
+constexpr int64_t kClipPiece = 4096;           // elements of a tensor; a workgroup takes a stretch of pieces
 constexpr int kClipTensors = 80;               // of one launch: their descriptions are its arguments
+constexpr int64_t kClipSums = 2048;            // workgroups of all launches together, about: each leaves a sum, and each adds up all of them
 
 struct ClipTensor {
     const void* data;
@@ -19,11 +20,11 @@ struct ClipTensor {
 struct ClipList {
     ClipTensor t[kClipTensors];                // none of them empty
     int32_t tensors, pieces;
-    int64_t piece0;                            // pieces of the launches before
+    int32_t wgs, sum0;                         // workgroups of the launch, and of the launches before
 };
-// sums[piece0 + i] = the squares of piece i
+// sums[sum0 + i] = the squares of workgroup i's pieces
 hipError_t launch_clip_sum(const ClipList& l, double* sums, hipStream_t s);
-// scales the pieces by the norm that all `pieces_all` sums give; norm_out may be null
-hipError_t launch_clip_scale(const ClipList& l, const double* sums, int32_t pieces_all, float max_norm, float* norm_out, hipStream_t s);
+// scales the pieces by the norm that all `sums_all` sums give; norm_out may be null
+hipError_t launch_clip_scale(const ClipList& l, const double* sums, int32_t sums_all, float max_norm, float* norm_out, hipStream_t s);
 
 }  // namespace gcoo

@@ -25,22 +25,38 @@ auto with_type(int type, F&& f)
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f, kRootHalf = 0.7071067811865476f, kDensity0 = 0.3989422804014327f;
 
+// 1 + erf(z / sqrt(2)) and exp(-z^2 / 2).  T of 2 bytes: by the rational approximation 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions, off by 1.5e-7 at the most, a thousandth of
+// what such a T is rounded by, and not by a difference for negative z, with the exponential that the slope needs anyway (14000 x 8000, bf16, the gradient through gelu: 150 us with the library's erf).
+template <typename T>
+__device__ __forceinline__ float erfc_and_exp(float z, float* e)
+{
+    *e = __expf(-0.5f * z * z);
+    if constexpr (sizeof(T) == 4) return 1.0f + erff(z * kRootHalf);
+    const float x = fabsf(z) * kRootHalf, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+    const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    return z < 0.0f ? p * *e : 2.0f - p * *e;
+}
+
+template <typename T>
 __device__ __forceinline__ float activate(int act, float z)
 {
     switch (act) {
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : z;
         case GCOO_ACT_SILU: return z * logistic(z);
-        case GCOO_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kRootHalf));
+        case GCOO_ACT_GELU: {
+            float e;
+            return 0.5f * z * erfc_and_exp<T>(z, &e);
+        }
         case GCOO_ACT_GELU_TANH: return z * logistic(2.0f * kGeluA * (z + kGeluB * z * z * z));
         default: return z;
     }
 }
 // the same for N values: one look at `act` for all of them
-template <int N>
+template <typename T, int N>
 __device__ __forceinline__ void activate_all(int act, float (&z)[N])
 {
     if (act == GCOO_ACT_NONE) return;
-#define GCOO_EACH(A) _Pragma("unroll") for (int u = 0; u < N; ++u) z[u] = activate(A, z[u]);
+#define GCOO_EACH(A) _Pragma("unroll") for (int u = 0; u < N; ++u) z[u] = activate<T>(A, z[u]);
     if (act == GCOO_ACT_RELU) { GCOO_EACH(GCOO_ACT_RELU) }
     else if (act == GCOO_ACT_SILU) { GCOO_EACH(GCOO_ACT_SILU) }
     else if (act == GCOO_ACT_GELU) { GCOO_EACH(GCOO_ACT_GELU) }
@@ -55,22 +71,33 @@ __device__ __forceinline__ float slope_of_gate(float z, float c, float q, float 
     return z != z ? z : s + c * s * (e * s) * (q + 3.0f * r * c2);
 }
 // dC act'(z)
+template <typename T>
 __device__ __forceinline__ float slope_times(int act, float z, float d)
 {
     switch (act) {
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : d;
         case GCOO_ACT_SILU: return slope_of_gate(z, fminf(fmaxf(z, -80.0f), 80.0f), 1.0f, 0.0f) * d;
-        case GCOO_ACT_GELU: return d * (0.5f * (1.0f + erff(z * kRootHalf)) + z * kDensity0 * __expf(-0.5f * z * z));
+        case GCOO_ACT_GELU: {
+            float e;
+            const float f = erfc_and_exp<T>(z, &e);
+            return d * (0.5f * f + z * kDensity0 * e);
+        }
         case GCOO_ACT_GELU_TANH: return slope_of_gate(z, fminf(fmaxf(z, -8.0f), 8.0f), 2.0f * kGeluA, 2.0f * kGeluA * kGeluB) * d;
         default: return d;
     }
 }
 
-__device__ __forceinline__ float wave_sum(float x)
+// d = d act'(z) for N values
+template <typename T, int N>
+__device__ __forceinline__ void slope_times_all(int act, const float (&z)[N], float (&d)[N])
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-    return x;
+    if (act == GCOO_ACT_NONE) return;
+#define GCOO_EACH(A) _Pragma("unroll") for (int u = 0; u < N; ++u) d[u] = slope_times<T>(A, z[u], d[u]);
+    if (act == GCOO_ACT_RELU) { GCOO_EACH(GCOO_ACT_RELU) }
+    else if (act == GCOO_ACT_SILU) { GCOO_EACH(GCOO_ACT_SILU) }
+    else if (act == GCOO_ACT_GELU) { GCOO_EACH(GCOO_ACT_GELU) }
+    else { GCOO_EACH(GCOO_ACT_GELU_TANH) }
+#undef GCOO_EACH
 }
 
 }  // namespace gcoo

@@ -56,7 +56,7 @@ __device__ __forceinline__ void layer_finish(const EpilogueArgs& e, int64_t r, i
 #pragma unroll
     for (int u = 0; u < COLS; ++u) x[u] += bias;
     if (e.Z) layer_put<T, COLS>(e.Z, r * e.ldz + jc, first, last, x);
-    activate_all<COLS>(e.activation, x);
+    activate_all<T, COLS>(e.activation, x);
 #pragma unroll
     for (int u = 0; u < COLS; ++u) x[u] += res[u];
     layer_put<T, COLS>(e.C, r * e.ldc + jc, first, last, x);

@@ -5,6 +5,9 @@
 
 namespace gcoo {
 
+constexpr int kFewThreads = 1024;
+constexpr int64_t kFewLdsBytes = 128 * 1024;
+
 // (registers for four waves of a SIMD, five with eight rows of B in flight: the epilogue and a lane's eight columns do not leave enough for eight)
 template <typename T, int LPR, bool WIDE, int AHEAD, int SUMS, RowsLong LONG>
 __global__ __launch_bounds__(kRowsThreads, AHEAD == 16 ? (LPR == 4 || (LPR == 16 && SUMS == 2) ? 3 : 4) : 5) void layer_rows(RowsArgs a, LayerIO<T, T> io, int32_t tiles, int32_t row_wgs, int32_t rpw, int32_t wave_row)
@@ -13,38 +16,76 @@ __global__ __launch_bounds__(kRowsThreads, AHEAD == 16 ? (LPR == 4 || (LPR == 16
     rows_item<LPR, WIDE, AHEAD, SUMS, LONG>(a, io, blockIdx.x, tiles, row_wgs, rpw, wave_row, RowsTurns{}, part);
 }
 
-// Few columns: LANES lanes share a row, each takes every LANES-th entry, four of them at a time, so that four rows of B are on their way; their sums are added up in a fixed tree.
-// A single token reads the entries and hardly anything else.
-template <typename T, int LANES, int N>
-__global__ __launch_bounds__(kRowsThreads) void layer_few(RowsArgs a, EpilogueArgs e)
+// Few columns: LANES lanes share a row, each takes four adjacent entries at a time with one load each of columns and values, GROUPS such on their way; their sums are added up in a fixed tree.
+// Bound for a single token: the entries, which are all that is read from memory.  The elements of B lie anywhere: from the vector cache a lane's takes a clock of its compute unit, so for many entries the whole
+// of B is brought to LDS first (HELD), which gives 64 lanes theirs in about five (8000 x 8000, 10 %, one token, bf16: 21 us from the cache, 13.4 so, of which reading the entries once at the rate of a large copy takes 10.4).
+template <typename T, int LANES, int N, int GROUPS, bool HELD>
+__global__ __launch_bounds__(HELD ? kFewThreads : kRowsThreads) void layer_few(RowsArgs a, EpilogueArgs e)
 {
+    constexpr int THREADS = HELD ? kFewThreads : kRowsThreads;
     const int lane = threadIdx.x % LANES;
-    const int64_t r = (int64_t)blockIdx.x * (kRowsThreads / LANES) + threadIdx.x / LANES;
-    if (r >= a.m) return;
+    const int64_t r = (int64_t)blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
     const uint32_t kmax = (uint32_t)(a.k - 1);
     const T* B = reinterpret_cast<const T*>(a.B);
     const int n = (int)a.N;
+    extern __shared__ __attribute__((aligned(16))) char few_smem[];
+    T* held = reinterpret_cast<T*>(few_smem);                              // B, its rows one behind the other
+    if constexpr (HELD) {
+        if (a.ldb == n) {
+            // (the last bytes of B by elements)
+            const int64_t all = a.k * n, vecs = all / 8;
+            for (int64_t i = threadIdx.x; i < vecs; i += THREADS) {
+                typename Adjacent<T, 8>::vec x = *reinterpret_cast<const typename Adjacent<T, 8>::vec*>(B + i * 8);
+                typedef T vec __attribute__((ext_vector_type(8)));
+                *reinterpret_cast<vec*>(held + i * 8) = x;
+            }
+            for (int64_t i = vecs * 8 + threadIdx.x; i < all; i += THREADS) held[i] = B[i];
+        } else {
+            for (int64_t c = threadIdx.x; c < a.k; c += THREADS)
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (j < n) held[c * n + j] = B[c * a.ldb + j];
+        }
+        __syncthreads();
+    }
+    if (r >= a.m) return;
     float sum[N] = {};
     const uint32_t end = (uint32_t)a.row_ptr[r + 1];                     // (unsigned: a step beyond the last of 2^31 entries stays a number)
-    for (uint32_t i = (uint32_t)a.row_ptr[r] + (uint32_t)lane; i < end; i += 4 * LANES) {
-        uint32_t c[4];
-        float v[4], b[4][N];
+    typedef uint32_t cols4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef float vals4 __attribute__((ext_vector_type(4), aligned(4)));
+    for (uint32_t i = (uint32_t)a.row_ptr[r] + 4 * (uint32_t)lane; i < end; i += 4 * LANES * GROUPS) {
+        uint32_t c[GROUPS][4];
+        float v[GROUPS][4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const bool in = i + q * LANES < end;
-            c[q] = in ? (uint32_t)a.cols[i + q * LANES] : 0xffffffffu;
-            v[q] = in ? a.vals[i + q * LANES] : 0.0f;
+        for (int g = 0; g < GROUPS; ++g) {
+            const uint32_t at = i + 4 * LANES * g;
+            if (at + 4 <= end) {
+                const cols4 x = *reinterpret_cast<const cols4*>(a.cols + at);
+                const vals4 y = *reinterpret_cast<const vals4*>(a.vals + at);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { c[g][q] = x[q]; v[g][q] = y[q]; }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bool in = at + q < end;
+                    c[g][q] = in ? (uint32_t)a.cols[at + q] : 0u;
+                    v[g][q] = in ? a.vals[at + q] : 0.0f;
+                }
+            }
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const T* row = B + (int64_t)(c[q] < kmax ? c[q] : kmax) * a.ldb;
+        for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-            for (int j = 0; j < N; ++j) b[q][j] = j < n && i + q * LANES < end ? widen(row[j]) : 0.0f;
-        }
+            for (int q = 0; q < 4; ++q) {
+                const bool in = i + 4 * LANES * g + q < end;
+                const uint32_t col = c[g][q] < kmax ? c[g][q] : kmax;
+                const T* row = HELD ? held + col * (uint32_t)n : B + (int64_t)col * a.ldb;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int j = 0; j < N; ++j) sum[j] = __builtin_fmaf(v[q], b[q][j], sum[j]);
+                for (int j = 0; j < N; ++j) {
+                    const float b = in && j < n ? widen(row[j]) : 0.0f;
+                    sum[j] = __builtin_fmaf(v[g][q], b, sum[j]);
+                }
+            }
     }
 #pragma unroll
     for (int j = 0; j < N; ++j)
@@ -75,14 +116,29 @@ hipError_t launch_layer_rows(const RowsArgs& a, const EpilogueArgs& e, int64_t N
     return launch_layer_rows_ahead<T, LPR, false, 16, SUMS>(a, e, N4, s);
 }
 
+template <typename T, int LANES, int N, int GROUPS>
+hipError_t launch_layer_few(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s)
+{
+    // (two workgroups to a compute unit, or one; and where the elements of B that are taken are worth the way to LDS)
+    const int64_t lds = a.k * a.N * (int64_t)sizeof(T);
+    if (lds > kFewLdsBytes || a.nnz * a.N < 2000000) {
+        layer_few<T, LANES, N, GROUPS, false><<<dim3((unsigned)((a.m + kRowsThreads / LANES - 1) / (kRowsThreads / LANES))), dim3(kRowsThreads), 0, s>>>(a, e);
+        return hipGetLastError();
+    }
+    static LdsLimit limit;
+    const auto kernel = &layer_few<T, LANES, N, GROUPS, true>;
+    const hipError_t err = limit.raise(reinterpret_cast<const void*>(kernel), (int)kFewLdsBytes);
+    if (err != hipSuccess) return err;
+    kernel<<<dim3((unsigned)((a.m + kFewThreads / LANES - 1) / (kFewThreads / LANES))), dim3(kFewThreads), (size_t)lds, s>>>(a, e);
+    return hipGetLastError();
+}
 template <typename T, int LANES>
 hipError_t launch_layer_few(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.m + kRowsThreads / LANES - 1) / (kRowsThreads / LANES))), threads(kRowsThreads);
-    if (a.N == 1) layer_few<T, LANES, 1><<<grid, threads, 0, s>>>(a, e);
-    else if (a.N <= 4) layer_few<T, LANES, 4><<<grid, threads, 0, s>>>(a, e);
-    else layer_few<T, LANES, 8><<<grid, threads, 0, s>>>(a, e);
-    return hipGetLastError();
+    if (a.N == 1) return launch_layer_few<T, LANES, 1, 4>(a, e, s);
+    if (a.N <= 4) return launch_layer_few<T, LANES, 4, 2>(a, e, s);
+    if constexpr (sizeof(T) == 2) return launch_layer_few<T, LANES, 8, 1>(a, e, s);
+    return hipErrorInvalidValue;
 }
 
 template <typename T>

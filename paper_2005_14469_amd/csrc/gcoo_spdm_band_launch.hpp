@@ -2,12 +2,10 @@
 #pragma once
 #include "gcoo_spdm_band_kernel.hpp"
 
-#include <atomic>
-
 namespace gcoo {
 
 // The instances: the cut, and how the rows of B are requested (gcoo_spdm_band_kernel.hpp).
-enum BandKind { kBandTallSpread, kBandTallFirst, kBandTallSecond, kBandWideSpread, kBandWideStep, kBandWideFirst, kBandWideSecond, kBandKinds };
+enum BandKind { kBandTallSpread, kBandTallFirst, kBandTallSecond, kBandWideSpread, kBandWideStep, kBandWideFirst, kBandWideSecond };
 struct BandLaunch {
     BandArgs a;
     RowsArgs rows;
@@ -17,24 +15,6 @@ struct BandLaunch {
 };
 // Checks what the kernel assumes and fills in the rest.
 hipError_t band_launch(const BandArgs& a, const RowsArgs& rows, BandLaunch* out);
-
-// More LDS than the default limit of a workgroup: asked for once per device and instance.
-struct BandLimits {
-    std::atomic<unsigned> done[kBandKinds][64] = {};
-    hipError_t raise(const void* kernel, BandKind kind)
-    {
-        int dev = -1;
-        hipError_t e = hipGetDevice(&dev);
-        if (e != hipSuccess) return e;
-        if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
-        if (!done[kind][dev].load(std::memory_order_acquire)) {
-            e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kBandLdsBytes);
-            if (e != hipSuccess) return e;
-            done[kind][dev].store(1u, std::memory_order_release);
-        }
-        return hipSuccess;
-    }
-};
 
 // b.launch<V, SPREAD, LATE>(stream) of b.l.kind
 template <class B>

@@ -5,9 +5,29 @@
 #include <stdint.h>
 #include <limits.h>
 
+#include <atomic>
+
 namespace gcoo {
 
 struct SchedClass;
+
+// More LDS than the default limit of a workgroup: asked for once per device and kernel.
+struct LdsLimit {
+    std::atomic<unsigned> done[64] = {};
+    hipError_t raise(const void* kernel, int bytes)
+    {
+        int dev = -1;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return e;
+        if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+        if (!done[dev].load(std::memory_order_acquire)) {
+            e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            if (e != hipSuccess) return e;
+            done[dev].store(1u, std::memory_order_release);
+        }
+        return hipSuccess;
+    }
+};
 
 struct SpdmArgs {
     const SchedClass* hdr;     // [g][nw][kMaxRun]

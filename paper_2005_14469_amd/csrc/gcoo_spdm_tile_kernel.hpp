@@ -25,8 +25,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <atomic>
-
 #include "gcoo_spdm_launch.hpp"
 
 namespace gcoo {
@@ -259,23 +257,5 @@ __device__ __forceinline__ void tile_item(const RowsArgs& a, int32_t row_wgs, in
 // Its launch; false where it does not serve the product.
 struct TileGrid { int64_t rows, wgs, total, lds; int32_t long_steps; };
 bool tile_grid(const RowsArgs& a, int64_t row_wgs, bool whole, TileGrid* g);
-
-// More LDS than the default limit of a workgroup: asked for once per device and kernel.
-struct TileLimit {
-    std::atomic<unsigned> done[64] = {};
-    hipError_t raise(const void* kernel)
-    {
-        int dev = -1;
-        hipError_t e = hipGetDevice(&dev);
-        if (e != hipSuccess) return e;
-        if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
-        if (!done[dev].load(std::memory_order_acquire)) {
-            e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kTileLdsBytes);
-            if (e != hipSuccess) return e;
-            done[dev].store(1u, std::memory_order_release);
-        }
-        return hipSuccess;
-    }
-};
 
 }  // namespace gcoo

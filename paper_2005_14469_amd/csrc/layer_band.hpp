@@ -95,8 +95,8 @@ struct LayerBand {
     template <int V, bool SPREAD, bool LATE>
     hipError_t launch(hipStream_t s) const
     {
-        static BandLimits limits;
-        const hipError_t err = limits.raise(reinterpret_cast<const void*>(&layer_band<T, V, SPREAD, LATE>), l.kind);
+        static LdsLimit limit;
+        const hipError_t err = limit.raise(reinterpret_cast<const void*>(&layer_band<T, V, SPREAD, LATE>), kBandLdsBytes);
         if (err != hipSuccess) return err;
         layer_band<T, V, SPREAD, LATE><<<l.blocks(), dim3(64 * kBandWaves), kBandLdsBytes, s>>>(l.a, l.rows, l.grid, LayerIO<float, T>{e});
         return hipGetLastError();

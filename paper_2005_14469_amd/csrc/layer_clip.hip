@@ -1,12 +1,13 @@
 // The norm of many gradients and their scaling to a given one, and its launcher.
 //
-// Two passes: squares are summed per piece of a tensor, then every workgroup adds up all pieces in their order (so that the bits are the same in each of them and on every
-// run, without a launch between the two) and scales its piece.  Squares and sums are in 64 bits: the square of an fp32 number is exact there and its sum can
+// Two passes over pieces of 4096 elements: a workgroup sums the squares of a stretch of pieces, then every workgroup adds up the sums of all (in one order, so that the bits are the same in
+// each of them and on every run, without a launch between the two) and scales its stretch.  Squares and sums are in 64 bits: the square of an fp32 number is exact there, and a sum can
 // neither overflow nor lose what a long fp32 sum does.
 //
+// Bound: memory.  The second pass goes through the pieces from the last to the first, so that it begins with what the memory-side cache (256 MB) still has of the first pass, and stores past the caches.
 // The tensors go with the launches, as arguments: nothing is copied to the device, and a captured call holds them itself.
 #include "gcoo_layer_clip.hpp"
-#include "gcoo_layer_device.hpp"
+#include "gcoo_layer_io.hpp"
 
 namespace gcoo {
 
@@ -21,14 +22,45 @@ __device__ __forceinline__ int clip_tensor(const ClipList& l, int32_t piece)
     return lo;
 }
 
-template <typename T>
-__device__ __forceinline__ double clip_squares(const T* x, int64_t n)
+// f(tensor, first element, elements) for the pieces of the workgroup; DOWN: from the last to the first, the workgroups too.
+template <bool DOWN, typename F>
+__device__ __forceinline__ void clip_pieces(const ClipList& l, F&& f)
 {
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += kClipThreads) {
-        const double v = (double)widen(x[i]);
-        sum = __builtin_fma(v, v, sum);
+    if (l.pieces == 0) return;
+    const int32_t wg = DOWN ? l.wgs - 1 - (int32_t)blockIdx.x : (int32_t)blockIdx.x;
+    const int32_t from = (int32_t)((int64_t)l.pieces * wg / l.wgs), to = (int32_t)((int64_t)l.pieces * (wg + 1) / l.wgs);
+    if (from >= to) return;
+    int x = clip_tensor(l, DOWN ? to - 1 : from);
+    for (int32_t i = 0; i < to - from; ++i) {
+        const int32_t piece = DOWN ? to - 1 - i : from + i;
+        if (DOWN) { while (l.t[x].first > piece) --x; }
+        else { while (x + 1 < l.tensors && l.t[x + 1].first <= piece) ++x; }
+        const int64_t at = (int64_t)(piece - l.t[x].first) * kClipPiece, left = l.t[x].count - at;
+        f(l.t[x], at, (int)(left < kClipPiece ? left : kClipPiece));
     }
+}
+
+template <typename T> constexpr int kClipVec = 16 / sizeof(T);
+template <typename T> constexpr int kClipSteps = kClipPiece / (kClipThreads * kClipVec<T>);       // 16-byte pieces of a thread
+
+template <typename T>
+__device__ __forceinline__ double clip_squares(const T* x, int n)
+{
+    constexpr int V = kClipVec<T>;
+    double sum = 0.0;
+    float v[kClipSteps<T>][V];
+#pragma unroll
+    for (int s = 0; s < kClipSteps<T>; ++s) {
+        const int at = (s * kClipThreads + (int)threadIdx.x) * V;
+        if (at + V <= n) layer_load<T, V>(x, at, v[s]);
+        else
+#pragma unroll
+            for (int u = 0; u < V; ++u) v[s][u] = at + u < n ? widen(x[at + u]) : 0.0f;
+    }
+#pragma unroll
+    for (int s = 0; s < kClipSteps<T>; ++s)
+#pragma unroll
+        for (int u = 0; u < V; ++u) sum = __builtin_fma((double)v[s][u], (double)v[s][u], sum);
     return sum;
 }
 
@@ -46,51 +78,71 @@ __device__ __forceinline__ double clip_block_sum(double sum, double* part)
 __global__ __launch_bounds__(kClipThreads) void clip_sum(ClipList l, double* sums)
 {
     __shared__ double part[kClipThreads / 64];
-    const ClipTensor& t = l.t[clip_tensor(l, (int32_t)blockIdx.x)];
-    const int64_t at = (int64_t)((int32_t)blockIdx.x - t.first) * kClipPiece, n = t.count - at < kClipPiece ? t.count - at : kClipPiece;
-    double sum;
-    if (t.type == GCOO_F32) sum = clip_squares(static_cast<const float*>(t.data) + at, n);
-    else if (t.type == GCOO_BF16) sum = clip_squares(static_cast<const bf16_t*>(t.data) + at, n);
-    else sum = clip_squares(static_cast<const f16_t*>(t.data) + at, n);
+    double sum = 0.0;
+    clip_pieces<false>(l, [&](const ClipTensor& t, int64_t at, int n) {
+        if (t.type == GCOO_F32) sum += clip_squares(static_cast<const float*>(t.data) + at, n);
+        else if (t.type == GCOO_BF16) sum += clip_squares(static_cast<const bf16_t*>(t.data) + at, n);
+        else sum += clip_squares(static_cast<const f16_t*>(t.data) + at, n);
+    });
     sum = clip_block_sum(sum, part);
-    if (threadIdx.x == 0) sums[l.piece0 + blockIdx.x] = sum;
+    if (threadIdx.x == 0) sums[l.sum0 + (int32_t)blockIdx.x] = sum;
 }
 
+// (x may be y: a thread loads what it stores itself)
 template <typename T>
-__device__ __forceinline__ void clip_scaled(const T* x, T* y, int64_t n, float factor)
+__device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t first, int n, float factor)
 {
-    for (int64_t i = threadIdx.x; i < n; i += kClipThreads) y[i] = narrow<T>(widen(x[i]) * factor);
+    constexpr int V = kClipVec<T>;
+    const T* x = static_cast<const T*>(data) + first;
+    T* y = static_cast<T*>(out) + first;
+    float v[kClipSteps<T>][V];
+#pragma unroll
+    for (int s = 0; s < kClipSteps<T>; ++s) {
+        const int at = (s * kClipThreads + (int)threadIdx.x) * V;
+        if (at + V <= n) layer_load<T, V>(x, at, v[s]);
+        else
+#pragma unroll
+            for (int u = 0; u < V; ++u) v[s][u] = at + u < n ? widen(x[at + u]) : 0.0f;
+    }
+#pragma unroll
+    for (int s = 0; s < kClipSteps<T>; ++s) {
+        const int at = (s * kClipThreads + (int)threadIdx.x) * V;
+#pragma unroll
+        for (int u = 0; u < V; ++u) v[s][u] *= factor;
+        if (at + V <= n) layer_store<T, V>(y, at, v[s]);
+        else
+#pragma unroll
+            for (int u = 0; u < V; ++u)
+                if (at + u < n) y[at + u] = narrow<T>(v[s][u]);
+    }
 }
 
-// The workgroups behind those of the list's pieces: none, or one that only writes the norm.
-__global__ __launch_bounds__(kClipThreads) void clip_scale(ClipList l, const double* sums, int32_t pieces_all, float max_norm, float* norm_out)
+__global__ __launch_bounds__(kClipThreads) void clip_scale(ClipList l, const double* sums, int32_t sums_all, float max_norm, float* norm_out)
 {
     __shared__ double part[kClipThreads / 64];
     double sum = 0.0;
-    for (int32_t i = threadIdx.x; i < pieces_all; i += kClipThreads) sum += sums[i];
+    for (int32_t i = threadIdx.x; i < sums_all; i += kClipThreads) sum += sums[i];
     const float norm = (float)sqrt(clip_block_sum(sum, part));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-    if ((int32_t)blockIdx.x >= l.pieces) return;
     const bool scales = !(max_norm >= norm + 1e-6f);                // (a NaN scales)
-    const ClipTensor& t = l.t[clip_tensor(l, (int32_t)blockIdx.x)];
-    if (!scales && t.data == t.out) return;
-    const int64_t at = (int64_t)((int32_t)blockIdx.x - t.first) * kClipPiece, n = t.count - at < kClipPiece ? t.count - at : kClipPiece;
     const float f = scales ? max_norm / (norm + 1e-6f) : 1.0f;
-    if (t.type == GCOO_F32) clip_scaled(static_cast<const float*>(t.data) + at, static_cast<float*>(t.out) + at, n, f);
-    else if (t.type == GCOO_BF16) clip_scaled(static_cast<const bf16_t*>(t.data) + at, static_cast<bf16_t*>(t.out) + at, n, f);
-    else clip_scaled(static_cast<const f16_t*>(t.data) + at, static_cast<f16_t*>(t.out) + at, n, f);
+    clip_pieces<true>(l, [&](const ClipTensor& t, int64_t at, int n) {
+        if (!scales && t.data == t.out) return;
+        if (t.type == GCOO_F32) clip_scaled<float>(t.data, t.out, at, n, f);
+        else if (t.type == GCOO_BF16) clip_scaled<bf16_t>(t.data, t.out, at, n, f);
+        else clip_scaled<f16_t>(t.data, t.out, at, n, f);
+    });
 }
 
 hipError_t launch_clip_sum(const ClipList& l, double* sums, hipStream_t s)
 {
-    if (l.pieces < 1) return hipSuccess;
-    clip_sum<<<dim3((unsigned)l.pieces), dim3(kClipThreads), 0, s>>>(l, sums);
+    clip_sum<<<dim3((unsigned)l.wgs), dim3(kClipThreads), 0, s>>>(l, sums);
     return hipGetLastError();
 }
-hipError_t launch_clip_scale(const ClipList& l, const double* sums, int32_t pieces_all, float max_norm, float* norm_out, hipStream_t s)
+hipError_t launch_clip_scale(const ClipList& l, const double* sums, int32_t sums_all, float max_norm, float* norm_out, hipStream_t s)
 {
-    if (l.pieces < 1 && !norm_out) return hipSuccess;
-    clip_scale<<<dim3((unsigned)(l.pieces > 0 ? l.pieces : 1)), dim3(kClipThreads), 0, s>>>(l, sums, pieces_all, max_norm, norm_out);
+    // (a list without pieces: one workgroup that writes the norm)
+    clip_scale<<<dim3((unsigned)(l.wgs > 0 ? l.wgs : 1)), dim3(kClipThreads), 0, s>>>(l, sums, sums_all, max_norm, norm_out);
     return hipGetLastError();
 }
 

@@ -2,8 +2,6 @@
 #include "gcoo_layer_io.hpp"
 #include "gcoo_spdm_tile_kernel.hpp"
 
-#include <atomic>
-
 namespace gcoo {
 
 template <typename T>
@@ -37,8 +35,8 @@ hipError_t launch_layer_tile(const RowsArgs& a, const EpilogueArgs& e, int64_t r
     if (a.ldb > 0x3fffffffLL || !tile_grid(a, row_wgs, whole, &g)) return hipErrorInvalidValue;
     return with_type(e.type, [&](auto t) {
         typedef decltype(t) T;
-        static TileLimit limit;
-        const hipError_t err = limit.raise(reinterpret_cast<const void*>(&layer_tile<T>));
+        static LdsLimit limit;
+        const hipError_t err = limit.raise(reinterpret_cast<const void*>(&layer_tile<T>), (int)kTileLdsBytes);
         if (err != hipSuccess) return err;
         layer_tile<T><<<dim3((unsigned)((g.total + 7) / 8 * 8)), dim3(kTileThreads), (size_t)g.lds, s>>>(a, e, (int32_t)g.wgs, (int32_t)g.rows, (int32_t)g.total, g.long_steps);
         return hipGetLastError();

@@ -2,8 +2,6 @@
 #include "gcoo_layer_values.hpp"
 #include "gcoo_layer_device.hpp"
 
-#include <atomic>
-
 namespace gcoo {
 
 // ---- from the caches: entry by entry ----
@@ -511,17 +509,9 @@ static hipError_t launch_tiles(const GradValuesArgs& a, const ValuesPlan& plan, 
     constexpr int TM = WM * MI * 32, TN = WN * 64, lds = 2 * (TM + TN) * 128;
     static_assert(64 * TN * 4 <= lds && TN == values_tile_cols(MI == 4), "the sums of 64 rows");
     const auto kernel = &values_tiles<T, WM, WN, MI>;
-    // more LDS than the default limit of a workgroup: asked for once per device
-    static std::atomic<unsigned> done[64];
-    int dev = -1;
-    hipError_t e = hipGetDevice(&dev);
+    static LdsLimit limit;
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
-    if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
-    if (!done[dev].load(std::memory_order_acquire)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (e != hipSuccess) return e;
-        done[dev].store(1u, std::memory_order_release);
-    }
     const int64_t tiles_m = (a.A.m + TM - 1) / TM, tiles_n = (a.A.k + TN - 1) / TN, total = tiles_m * tiles_n * plan.parts;
     if (total > 0x7ffffff0LL) return hipErrorInvalidConfiguration;
     const int64_t steps = (a.N * (int64_t)sizeof(T) + 127) / 128;

@@ -47,8 +47,8 @@ struct PlainBand {
     template <int V, bool SPREAD, bool LATE>
     hipError_t launch(hipStream_t s) const
     {
-        static BandLimits limits;
-        const hipError_t e = limits.raise(reinterpret_cast<const void*>(&spdm_band<V, SPREAD, LATE>), l.kind);
+        static LdsLimit limit;
+        const hipError_t e = limit.raise(reinterpret_cast<const void*>(&spdm_band<V, SPREAD, LATE>), kBandLdsBytes);
         if (e != hipSuccess) return e;
         spdm_band<V, SPREAD, LATE><<<l.blocks(), dim3(64 * kBandWaves), kBandLdsBytes, s>>>(l.a, l.rows, l.grid);
         return hipGetLastError();

@@ -24,8 +24,8 @@ hipError_t launch_spdm_rows_tile(const RowsArgs& a, int64_t row_wgs, bool whole,
 {
     TileGrid g;
     if ((uint64_t)a.k * (uint64_t)a.ldb * 4u > kRowsMaxBytes || !tile_grid(a, row_wgs, whole, &g)) return hipErrorInvalidValue;
-    static TileLimit limit;
-    const hipError_t e = limit.raise(reinterpret_cast<const void*>(&spdm_rows_tile));
+    static LdsLimit limit;
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(&spdm_rows_tile), (int)kTileLdsBytes);
     if (e != hipSuccess) return e;
     spdm_rows_tile<<<dim3((unsigned)((g.total + 7) / 8 * 8)), dim3(kTileThreads), (size_t)g.lds, s>>>(a, (int32_t)g.wgs, (int32_t)g.rows, (int32_t)g.total, g.long_steps);
     return hipGetLastError();

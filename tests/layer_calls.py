@@ -78,6 +78,10 @@ def refusals():
                dict(dC=AT + 2), dict(Z=AT + 1, type=BF16), dict(dZ=AT + 1, type=F16), dict(db=AT + 2), dict(dZ=2 * AT, lddz=10)):
         H.refused(H.grad(**kw), kw)
     assert H.grad(act=0, Z=None, ldz=0, dZ=None, lddz=0) == OK and H.launches()
+    wide = dict(m=1, N=70001, ldz=70001, lddc=70001, lddz=70001)
+    need = H.L.gcoo_epilogue_grad_bytes(1, 70001)
+    assert need > 0 and H.grad(**wide, bytes=need) == OK and len(H.launches()) == 2
+    assert H.grad(**wide, bytes=need - 1) == ENOMEM and not H.launches()
     for kw in (dict(m=0), dict(dZ=None, db=None), dict(N=0, dC=None, Z=None, db=None)):
         assert H.grad(**kw) == OK and not H.launches(), kw
     assert H.grad(N=0, dC=None, Z=None) == OK and len(H.launches()) == 1
@@ -93,7 +97,7 @@ def refusals():
     for tensors in ([(AT, AT, -1, F32)], [(AT, AT, 10, 3)], [(None, AT, 10, F32)], [(AT, None, 10, F32)], [(AT + 2, AT + 2, 10, F32)], [(AT, AT + 1, 10, F16)], [t, t], [t, (AT + 396, AT + 396, 10, F32)],
                     [(AT, AT + 4, 100, F32)], [(AT, 2 * AT, 100, F32), (2 * AT + 8, 3 * AT, 10, F32)], [(AT, 2 * AT, 100, F32), (3 * AT, 2 * AT + 198, 10, BF16)], [(AT, AT, 1 << 61, F32)], [(AT, AT, 1 << 50, F32)]):
         H.refused(H.clip(*tensors), tensors)
-    for kw in (dict(norm=None), dict(norm=AT + 2), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(work=None)):
+    for kw in (dict(norm=None), dict(norm=AT + 2), dict(norm=AT + 396), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(work=None)):
         H.refused(H.clip(t, **kw), kw)
     assert H.clip((AT, 2 * AT, 100, F32), (AT, 3 * AT, 100, F32), (AT + 400, AT + 400, 5, F32)) == OK and H.launches()      # (read twice, written once each)
     assert H.clip((None, None, 0, F32), max_norm=float("inf"), work=None, bytes=0) == OK and len(H.launches()) == 1
