@@ -76,6 +76,7 @@ class _ByCtypes:
         lib().gcoo_free(handle)
 
     from_csr_device = from_csr_host = from_csr_device_static = from_dense = spdm = staticmethod(lambda *args: None)
+    spdm_epilogue = epilogue_grad = grad_values = clip_grad_norm = staticmethod(lambda *args: None)
 
 
 def lib():
@@ -156,7 +157,8 @@ def lib():
         if calls is not _ByCtypes:
             calls.bind(*(C.cast(getattr(L, name), vp).value for name in
                           ("gcoo_device_bytes", "gcoo_from_csr", "gcoo_from_csr_device", "gcoo_from_csr_device_static", "gcoo_dense_count_bytes", "gcoo_dense_count",
-                           "gcoo_from_dense_counted", "gcoo_spdm_variant", "gcoo_free")))
+                           "gcoo_from_dense_counted", "gcoo_spdm_variant", "gcoo_free", "gcoo_spdm_epilogue_bytes", "gcoo_spdm_epilogue", "gcoo_epilogue_grad_bytes", "gcoo_epilogue_grad",
+                           "gcoo_spdm_grad_values_bytes", "gcoo_spdm_grad_values", "gcoo_clip_grad_norm_bytes", "gcoo_clip_grad_norm")))
         _calls = calls
         _lib = L
         if calls is _ByCtypes:
@@ -512,6 +514,13 @@ def gcoo_spdm_epilogue(A: GcooMatrix, B: torch.Tensor, bias: torch.Tensor | None
 
     B [k, N], residual, C_out and Z_out [m, N]: fp32, bfloat16 or float16, one type, unit column stride; bias [m] fp32; activation: ACT_* or a name of
     ACTIVATIONS.  C_out may be the residual.  The gradient of B is the same call with the transpose of A."""
+    if stream is None and B.is_cuda:
+        m, k = A._mk or A.shape
+        got = (_calls or _module()).spdm_epilogue(A._h or A._address(), A.buf, m, k, B, bias, _activation(activation), residual, C_out, Z_out, _raw_stream(B.get_device()))
+        if got is not None:
+            if type(got) is int:
+                raise GcooError(got, "gcoo_spdm_epilogue")
+            return got
     assert B.is_cuda and B.dim() == 2 and B.dtype in _TYPES
     m, k = A.shape
     N, d = B.shape[1], B.get_device()
@@ -546,6 +555,12 @@ def gcoo_epilogue_grad(dC: torch.Tensor, Z: torch.Tensor | None = None, activati
 
     Z: what gcoo_spdm_epilogue() stored in Z_out; not needed without an activation, where dZ is dC (and is returned as dC itself unless dZ_out is given).
     dZ_out may be dC."""
+    if stream is None and dC.is_cuda:
+        got = (_calls or _module()).epilogue_grad(dC, Z, _activation(activation), dZ_out, _raw_stream(dC.get_device()))
+        if got is not None:
+            if type(got) is int:
+                raise GcooError(got, "gcoo_epilogue_grad")
+            return got
     assert dC.is_cuda and dC.dim() == 2 and dC.dtype in _TYPES
     (m, N), d, act = dC.shape, dC.get_device(), _activation(activation)
     lddc = _rows_of(dC, m, N, dC.dtype, d)
@@ -570,6 +585,13 @@ def gcoo_epilogue_grad(dC: torch.Tensor, Z: torch.Tensor | None = None, activati
 
 def gcoo_spdm_grad_values(A: GcooMatrix, dZ: torch.Tensor, B: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The gradient of the stored values of A, from that of Z = A x B: [nnz] fp32, in the order of the CSR arrays that A came from (of a dense A: row by row)."""
+    if stream is None and B.is_cuda:
+        m, k = A._mk or A.shape
+        got = (_calls or _module()).grad_values(A._h or A._address(), A.buf, m, k, A.nnz, dZ, B, out, _raw_stream(B.get_device()))
+        if got is not None:
+            if type(got) is int:
+                raise GcooError(got, "gcoo_spdm_grad_values")
+            return got
     assert dZ.is_cuda and B.is_cuda and dZ.dim() == 2 and B.dim() == 2 and B.dtype in _TYPES
     m, k = A.shape
     N, d = B.shape[1], B.get_device()
@@ -598,6 +620,12 @@ def gcoo_clip_grad_norm(tensors, max_norm: float, out=None, stream=None) -> torc
     tensors = list(tensors)
     out = tensors if out is None else list(out)
     assert tensors and len(out) == len(tensors)
+    if stream is None and tensors[0].is_cuda:
+        got = (_calls or _module()).clip_grad_norm(tensors, out, max_norm, _raw_stream(tensors[0].get_device()))
+        if got is not None:
+            if type(got) is int:
+                raise GcooError(got, "gcoo_clip_grad_norm")
+            return got
     d = tensors[0].get_device()
     arr = (Gradient * len(tensors))()
     for g, t, o in zip(arr, tensors, out):

@@ -480,8 +480,39 @@ def test_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
-def test_refuses():
+class _Nothing:
+    """In the place of the extension module: serves no call, so that all go by ctypes."""
+
+    def __getattr__(self, name):
+        return (lambda h: binding.lib().gcoo_free(h)) if name == "free" else (lambda *args: None)
+
+
+def test_same_bits_with_and_without_the_module(monkeypatch):
+    print("calls: with and without the module", flush=True)
+    m, k, N = 300, 310, 70
+    arrays = csr(m, k, 0.1, 12)
+    perm = transpose(m, k, arrays)
+    rng = np.random.default_rng(6)
+    results = []
+    for _ in range(2):
+        for dtype in TYPES.values():
+            gen = np.random.default_rng(7)
+            X, dY, R, bias = normal(gen, k, N, dtype=dtype), normal(gen, m, N + 3, dtype=dtype)[:, 1:N + 1], normal(gen, m, N, dtype=dtype), normal(gen, m)
+            out = training_step(m, k, [torch.from_numpy(x).to(DEV) for x in arrays], perm, X, dY, bias, R, "gelu", dtype)
+            plain = binding.gcoo_epilogue_grad(dY)
+            assert plain[0] is dY
+            results.append([*out, plain[1], binding.gcoo_clip_grad_norm([X.contiguous(), R], 0.1, out=[torch.empty_like(X), torch.empty_like(R)])])
+        monkeypatch.setattr(binding, "_calls", _Nothing())
+    for a, b in zip(results[:3], results[3:], strict=True):
+        assert all(torch.equal(x, y) for x, y in zip(a, b, strict=True))
+
+
+@pytest.mark.parametrize("module", [True, False])
+def test_refuses(module, monkeypatch):
     print("refusals", flush=True)
+    binding.lib()
+    if not module:
+        monkeypatch.setattr(binding, "_calls", _Nothing())
     arrays = csr(30, 40, 0.2, 1)
     A = matrix(30, 40, arrays)
     freed = matrix(30, 40, arrays)
