@@ -1808,11 +1808,13 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
     if (N < 16 / size) return {kProductRows, 0, 0};
     const int64_t N4 = size == 4 ? N : (N + 1) / 2;
     const bool lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0;
-    const double slow = odd_elements(B, ldb, N, type) ? 2.0 : 1.0;
+    const double slow = odd_elements(B, ldb, N, type) ? 2.0 : 1.0;           // (read by 64-bit addresses, and inside lines)
     ProductPlan p{kProductRows, 0, 0};
     double best = slow * rows_time(m, k, nnz, N4, lines);
+    // (2-byte elements: row by row about 1.45 of what a matrix of half as many 4-byte ones takes where it stays in the caches, since they have to be widened for every entry; us, row by row and on tiles, bf16: 2000 x 2000,
+    // N = 2000, 2 %: 25.1 23.9, 5 %: 46.5 38.7; 1000 x 1000, N = 512, 5 %: 9.5 10.0)
     const TilePlan& tile = tile_plan(m, k, nnz, N);
-    if (tile.row_wgs > 0 && tile.time < 0.85 * slow * few_columns_rows_time(m, k, nnz, N4, lines)) {
+    if (tile.row_wgs > 0 && tile.time < 0.85 * (size == 4 ? 1.0 : 1.45 * slow) * few_columns_rows_time(m, k, nnz, N4, lines)) {
         p.kernel = kProductTile;
         best = std::min(best, tile.time + 1.0);
     }

@@ -6,7 +6,7 @@ namespace gcoo {
 
 // ---- from the caches: entry by entry ----
 //
-// Sixteen lanes (a slot) are on a row of A: each holds P pieces of 16 bytes of the row of dZ in registers, in fp32, and takes the same pieces of the row of B of every entry, so that an
+// Sixteen lanes (a slot) are on a row of A: each holds P pieces of 16 bytes of the row of dZ in registers and takes the same pieces of the row of B of every entry, so that an
 // entry costs P loads and 16 lanes x P pieces of multiply-adds.  Sixteen entries leave sixteen partial sums in every lane; they are added up by exchanging halves (the
 // lanes that keep the upper eight sums give the lower eight to those that keep these, and so on), 45 instructions for sixteen entries instead of 128, after which lane i holds the sum of entry i.
 // A wave has four rows beside each other, or all four slots on one row where it is long or rows are few.
@@ -45,6 +45,46 @@ template <typename T> struct Piece {
 };
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// A lane's 16 bytes of a row of dZ, and their product with 16 bytes of a row of B, added to s.  bf16 stays in pairs: an instruction adds two exact products to a sum in fp32 and rounds once (checked against 64 bits, denormal
+// numbers among them; the one for fp16 loses bits of those, where a multiply-add that takes one operand in fp16 does not).  With both operands widened, two instructions to an element, the
+// vector instructions took 80 % of the time (8000 x 8000, 0.5 %, N = 8000: 292 us).
+template <typename T> struct Held {
+    float x[16 / sizeof(T)];
+    __device__ __forceinline__ void set(const u32x4& w)
+    {
+        const typename Piece<T>::vec v = __builtin_bit_cast(typename Piece<T>::vec, w);
+#pragma unroll
+        for (int u = 0; u < Piece<T>::kElements; ++u) x[u] = widen((T)v[u]);
+    }
+    __device__ __forceinline__ float times(const u32x4& w, float s) const
+    {
+        const typename Piece<T>::vec v = __builtin_bit_cast(typename Piece<T>::vec, w);
+#pragma unroll
+        for (int u = 0; u < Piece<T>::kElements; ++u) s = __builtin_fmaf(x[u], widen((T)v[u]), s);
+        return s;
+    }
+};
+template <> struct Held<bf16_t> {
+    typedef bf16_t pair __attribute__((ext_vector_type(2)));
+    pair x[4];
+    static __device__ __forceinline__ pair of(const u32x4& w, int u)
+    {
+        const uint32_t word = w[u];
+        return __builtin_bit_cast(pair, word);
+    }
+    __device__ __forceinline__ void set(const u32x4& w)
+    {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = of(w, u);
+    }
+    __device__ __forceinline__ float times(const u32x4& w, float s) const
+    {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_fdot2_f32_bf16(x[u], of(w, u), s, false);
+        return s;
+    }
+};
+
 // B for a tile: by a buffer descriptor, or (ANY) by addresses in 64 bits, which serve a B of 4 GB and more and elements at odd places.
 struct ValuesB {
     __amdgpu_buffer_rsrc_t rsrc;
@@ -81,9 +121,8 @@ __device__ __forceinline__ void values_load(uint32_t off, const Pieces<T, P>& pc
 }
 
 template <typename T, int P, bool PART, bool ANY, int FROM, int CNT>
-__device__ __forceinline__ void values_batch(uint32_t off, const Pieces<T, P>& pc, const ValuesB& B, const float (&z)[P * Piece<T>::kElements], float (&sums)[16])
+__device__ __forceinline__ void values_batch(uint32_t off, const Pieces<T, P>& pc, const ValuesB& B, const Held<T> (&z)[P], float (&sums)[16])
 {
-    constexpr int E = Piece<T>::kElements;
     u32x4 b[CNT * P];
     values_load<T, P, PART, ANY, FROM, CNT>(off, pc, B, b);
 #pragma unroll
@@ -93,9 +132,7 @@ __device__ __forceinline__ void values_batch(uint32_t off, const Pieces<T, P>& p
         for (int q = 0; q < P; ++q) {
             u32x4 w = b[i * P + q];
             if constexpr (PART) w &= pc.keep[q];
-            const typename Piece<T>::vec x = __builtin_bit_cast(typename Piece<T>::vec, w);
-#pragma unroll
-            for (int u = 0; u < E; ++u) s = __builtin_fmaf(z[q * E + u], widen((T)x[u]), s);
+            s = z[q].times(w, s);
         }
         sums[FROM + i] = s;
     }
@@ -139,8 +176,7 @@ struct ValuesTile {
             }
         }
     }
-    // the row of dZ, in fp32
-    __device__ __forceinline__ void row(int64_t r, float (&z)[P * E]) const
+    __device__ __forceinline__ void row(int64_t r, Held<T> (&z)[P]) const
     {
         const char* src = reinterpret_cast<const char*>(static_cast<const T*>(a.dZ) + r * a.lddz + (j0 > a.N - E ? a.N - E : j0));
 #pragma unroll
@@ -148,9 +184,7 @@ struct ValuesTile {
             u32x4 w = 0u;
             if (!(PART && pc.none[q])) __builtin_memcpy(&w, src + pc.at[q], 16);
             if constexpr (PART) w &= pc.keep[q];
-            const typename Piece<T>::vec x = __builtin_bit_cast(typename Piece<T>::vec, w);
-#pragma unroll
-            for (int u = 0; u < E; ++u) z[q * E + u] = widen((T)x[u]);
+            z[q].set(w);
         }
     }
     __device__ __forceinline__ uint32_t offset(uint32_t e, uint32_t end) const
@@ -160,7 +194,7 @@ struct ValuesTile {
         return ANY ? in : in * pitch;
     }
     // The entries beg, beg + step, ... below end by sixteens, for each slot its own (every lane of the wave calls it).  (Unsigned: a step beyond the last of 2^31 entries stays a number.)
-    __device__ __forceinline__ void entries(uint32_t beg, uint32_t end, uint32_t step, const float (&z)[P * E]) const
+    __device__ __forceinline__ void entries(uint32_t beg, uint32_t end, uint32_t step, const Held<T> (&z)[P]) const
     {
         uint32_t e = beg + (uint32_t)(lane & 15);
         uint32_t next = offset(e, end);
@@ -198,7 +232,7 @@ struct ValuesTile {
         const int64_t m = a.A.m, r = one ? r0 : r0 + slot;
         int32_t beg = 0, end = 0;
         if (r < m) { beg = a.A.start[r]; end = a.A.start[r + 1]; }
-        float z[P * E];
+        Held<T> z[P];
         if (!one) {
             // a row of more entries than the others of the wave together would have them wait: all slots take it
             const int32_t n = end - beg;
