@@ -1799,23 +1799,29 @@ RowsView rows_view(const gcoo_matrix* A)
 }
 int hip_failed(hipError_t e, const char* what) { return hip_fail(e, what); }
 
-// The times are those of the products in fp32.  Row by row a B of 2-byte elements is one of half as many columns, and twice that where it has to be read by 64-bit addresses; the bands are of fp32, which costs a pass over B.
+// The times are those of the products in fp32.  Row by row a B of 2-byte elements is one of half as many columns; rows at odd places, which are read by 64-bit addresses, take 1.4 times as long (us, N = 513,
+// bf16, leading dimensions of 513 and 520: 8000 x 8000, 5 %: 308 210; 1 %: 73 54), or a pass that copies them.  The bands are of fp32, which costs a pass over B as well.
 ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64_t N, int type)
 {
     if (A->inner) A = A->inner;
     const int64_t m = A->m, k = A->k, nnz = A->nnz, size = (int64_t)type_bytes(type);
     if (nnz == 0 || k < 1) return {kProductNone, 0, 0};
     if (N < 16 / size) return {kProductRows, 0, 0};
-    const int64_t N4 = size == 4 ? N : (N + 1) / 2;
-    const bool lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0;
-    const double slow = odd_elements(B, ldb, N, type) ? 2.0 : 1.0;           // (read by 64-bit addresses, and inside lines)
+    const int64_t N4 = size == 4 ? N : (N + 1) / 2, padded = (N + 63) / 64 * 64;
+    const bool lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0, odd = odd_rows(B, ldb, type);
     ProductPlan p{kProductRows, 0, 0};
-    double best = slow * rows_time(m, k, nnz, N4, lines);
+    const double even = rows_time(m, k, nnz, N4, lines), copied = 2.0 + 4.0 * (double)k * (double)N / 4.5e6;
+    double best = odd ? 1.4 * even : even;
+    if (odd && even + copied < best && (uint64_t)k * (uint64_t)padded * 2u <= kRowsMaxBytes) {
+        p.ldw = padded;
+        p.work = al((size_t)k * (size_t)padded * 2);
+        best = even + copied;
+    }
     // (2-byte elements: row by row about 1.45 of what a matrix of half as many 4-byte ones takes where it stays in the caches, since they have to be widened for every entry; us, row by row and on tiles, bf16: 2000 x 2000,
     // N = 2000, 2 %: 25.1 23.9, 5 %: 46.5 38.7; 1000 x 1000, N = 512, 5 %: 9.5 10.0)
     const TilePlan& tile = tile_plan(m, k, nnz, N);
-    if (tile.row_wgs > 0 && tile.time < 0.85 * (size == 4 ? 1.0 : 1.45 * slow) * few_columns_rows_time(m, k, nnz, N4, lines)) {
-        p.kernel = kProductTile;
+    if (tile.row_wgs > 0 && tile.time < 0.85 * (size == 4 ? 1.0 : (odd ? 2.0 : 1.45)) * few_columns_rows_time(m, k, nnz, N4, lines)) {
+        p = {kProductTile, 0, 0};
         best = std::min(best, tile.time + 1.0);
     }
     const BandPlan band = A->L.band;
@@ -1824,7 +1830,7 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
         const bool aligned = N % 4 == 0 && ldw % 4 == 0 && (size == 2 || reinterpret_cast<uintptr_t>(B) % 16 == 0);
         const double t = band_time(m, k, nnz, N, band, size == 2 || lines) + (size == 2 ? 2.0 + 6.0 * (double)k * (double)N / 4.5e6 : 0.0);
         if ((aligned || N >= 64 * band.v) && (uint64_t)k * (uint64_t)ldw * 4u <= kRowsMaxBytes && t < best) {
-            p.kernel = kProductBand;
+            p = {kProductBand, 0, 0};
             if (size == 2) { p.ldw = ldw; p.work = al((size_t)k * (size_t)ldw * 4); }
         }
     }
@@ -1837,10 +1843,9 @@ hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const v
     if (plan.kernel == kProductNone) return launch_epilogue(A->m, N, e, s);
     const float* wide = static_cast<const float*>(B);
     if (plan.work > 0) {
-        float* to = static_cast<float*>(work);
-        const hipError_t err = launch_widen(B, ldb, e.type, to, plan.ldw, A->k, N, s);
+        const hipError_t err = plan.kernel == kProductBand ? launch_widen(B, ldb, e.type, static_cast<float*>(work), plan.ldw, A->k, N, s) : launch_realign(B, ldb, work, plan.ldw, A->k, N, s);
         if (err != hipSuccess) return err;
-        wide = to;
+        wide = static_cast<const float*>(work);
         ldb = plan.ldw;
     }
     const RowsArgs rows = rows_args(A, wide, ldb, N, nullptr, N);

@@ -32,20 +32,21 @@ struct EpilogueArgs {
     int32_t type, activation;
 };
 
-// dst[r][0 .. N) = src[r][0 .. N) in fp32; ldd a multiple of 8
+// dst[r][0 .. N) = src[r][0 .. N) of 2-byte elements, in fp32, or as they are; ldd a multiple of 8
+hipError_t launch_realign(const void* src, int64_t lds, void* dst, int64_t ldd, int64_t rows, int64_t N, hipStream_t s);
 hipError_t launch_widen(const void* src, int64_t lds, int type, float* dst, int64_t ldd, int64_t rows, int64_t N, hipStream_t s);
 // the epilogue of a matrix without entries
 hipError_t launch_epilogue(int64_t m, int64_t N, const EpilogueArgs& e, hipStream_t s);
 
 // Which kernel a product with its epilogue runs: none has entries, row by row (and few columns), on tiles of B in LDS, or by the sixteen-wave kernel, for which a B of 2-byte elements is
-// widened into `work` bytes of the caller's, rows ldw elements apart.
+// widened into `work` bytes of the caller's, rows ldw elements apart (and row by row, where that pays for rows at odd places, copied there).
 enum ProductKernel { kProductNone, kProductRows, kProductTile, kProductBand };
 struct ProductPlan { ProductKernel kernel; int64_t ldw; size_t work; };
 ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64_t N, int type);
 hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const void* B, int64_t ldb, int64_t N, const EpilogueArgs& e, void* work, hipStream_t s);
 
-// Elements of 2 bytes at places that 16-byte buffer loads, which want multiples of 4, do not take: they are read by 64-bit addresses.
-inline bool odd_elements(const void* B, int64_t ldb, int64_t N, int type) { return type != GCOO_F32 && (reinterpret_cast<uintptr_t>(B) % 4 != 0 || ldb % 2 != 0 || N % 2 != 0); }
+// Rows of 2-byte elements at places that 16-byte buffer loads, which want multiples of 4, do not take: they are read by 64-bit addresses.
+inline bool odd_rows(const void* B, int64_t ldb, int type) { return type != GCOO_F32 && (reinterpret_cast<uintptr_t>(B) % 4 != 0 || ldb % 2 != 0); }
 
 // RowsArgs::B and BandArgs::B point to elements of e.type (of the bands: to fp32); C is in e.
 hipError_t launch_layer_rows_f32(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s);

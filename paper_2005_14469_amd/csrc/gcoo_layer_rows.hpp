@@ -150,7 +150,7 @@ hipError_t launch_layer_rows_of(const RowsArgs& a, const EpilogueArgs& e, hipStr
     RowsArgs as4 = a;
     if (sizeof(T) == 2) { as4.N = (a.N + 1) / 2; as4.ldb = (a.ldb + 1) / 2; }
     // Beyond the offsets of a buffer descriptor, or at places that its loads do not take: 64-bit addresses.
-    if (odd_elements(a.B, a.ldb, a.N, e.type) || (uint64_t)a.k * (uint64_t)a.ldb * sizeof(T) > kRowsMaxBytes) return launch_layer_rows_ahead<T, 16, true, 16, 1>(a, e, as4.N, s);
+    if (odd_rows(a.B, a.ldb, e.type) || (uint64_t)a.k * (uint64_t)a.ldb * sizeof(T) > kRowsMaxBytes) return launch_layer_rows_ahead<T, 16, true, 16, 1>(a, e, as4.N, s);
     RowsWidth w = rows_width(as4);
     // Many rows of B and more entries than a narrow wave has on their way: 16 lanes to a row, not 32, whose eight columns in two sums leave no registers for a fifth wave and whose tiles of 512 bytes have to share the L2 with
     // what the epilogue reads (us, 32 and 16: bf16, N = 8000: 5500 x 5500, 0.3 %: 128 111; 6500, 0.6 %: 222 201; 8000, 0.3 %: 218 189, 0.6 %: 324 285; N = 2000: 8000, 0.3 %: 65 60; fp16, N = 8000: 6500, 0.3 %:

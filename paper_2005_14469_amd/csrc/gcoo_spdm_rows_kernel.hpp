@@ -213,7 +213,7 @@ struct RowsTile {
     const RowsArgs& a;
     const IO& io;
     int lane, slot, sl;
-    int32_t N, jb, lane_j;
+    int32_t N, jb, lane_j;                             // N: columns that are loaded; of 2-byte elements an even number, of which the last may be nobody's: it lies in the padding of a row, or behind the last row in the same four bytes as its last element
     uint32_t kmax, ldb4, c_word, ldc_word;
     RowsB B;
     __device__ __forceinline__ RowsTile(const RowsArgs& args, const IO& out, int32_t tile) : a(args), io(out)
@@ -223,14 +223,14 @@ struct RowsTile {
         sl = lane % LPR;
         const int64_t j0 = (int64_t)tile * (LPR * COLS);                 // first column of the tile, less up to `moved` (place())
         // The descriptor starts at or before the first column any lane of the tile loads.
-        const int64_t first = j0 - a.moved < 0 ? 0 : (j0 - a.moved < a.N - COLS ? j0 - a.moved : a.N - COLS);
+        const int64_t all = BYTES == 2 && !WIDE ? (a.N + 1) / 2 * 2 : a.N, first = j0 - a.moved < 0 ? 0 : (j0 - a.moved < all - COLS ? j0 - a.moved : all - COLS);
         const char* bbase = reinterpret_cast<const char*>(a.B) + first * BYTES;
-        const uint64_t bytes = ((uint64_t)(a.k - 1) * (uint64_t)a.ldb + (uint64_t)a.N - (uint64_t)first) * BYTES;
+        const uint64_t bytes = ((uint64_t)(a.k - 1) * (uint64_t)a.ldb + (uint64_t)all - (uint64_t)first) * BYTES;
         B.rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(bbase), 0, (int)(uint32_t)bytes, 0x00027000);
         B.base = bbase;
         B.pitch = (uint64_t)a.ldb * BYTES;
         jb = (int32_t)first;
-        N = (int32_t)a.N;
+        N = (int32_t)all;
         lane_j = (int32_t)j0 + sl * COLS;
         ldb4 = (uint32_t)a.ldb * BYTES;
         kmax = (uint32_t)(a.k - 1);
@@ -248,6 +248,7 @@ struct RowsTile {
         pl.jc = want < 0 ? 0 : (want > N - COLS ? N - COLS : want);
         pl.first = want - pl.jc < 0 ? 0 : want - pl.jc;
         pl.last = want - pl.jc + COLS;
+        if constexpr (BYTES == 2 && !WIDE) pl.last = pl.last < (int32_t)a.N - pl.jc ? pl.last : (int32_t)a.N - pl.jc;
         return pl;
     }
     template <int KEPT>

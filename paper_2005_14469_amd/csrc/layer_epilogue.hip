@@ -25,6 +25,21 @@ __global__ __launch_bounds__(kPassThreads) void layer_widen(const T* __restrict_
     }
 }
 
+__global__ __launch_bounds__(kPassThreads) void layer_realign(const uint16_t* __restrict__ src, int64_t lds, uint16_t* __restrict__ dst, int64_t ldd, int64_t rows, int64_t N)
+{
+    const int64_t j = ((int64_t)blockIdx.x * kPassThreads + threadIdx.x) * 8;
+    if (j >= N) return;
+    typedef uint16_t vec __attribute__((ext_vector_type(8)));
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        vec x;
+        if (j + 8 <= N) x = *reinterpret_cast<const Adjacent<uint16_t, 8>::vec*>(src + r * lds + j);
+        else
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = j + u < N ? src[r * lds + j + u] : (uint16_t)0;
+        *reinterpret_cast<vec*>(dst + r * ldd + j) = x;
+    }
+}
+
 // A matrix without entries.
 template <typename T>
 __global__ __launch_bounds__(kPassThreads) void layer_no_entries(int64_t m, int64_t N, EpilogueArgs e)
@@ -50,6 +65,12 @@ hipError_t launch_widen(const void* src, int64_t lds, int type, float* dst, int6
             return hipGetLastError();
         }
     });
+}
+
+hipError_t launch_realign(const void* src, int64_t lds, void* dst, int64_t ldd, int64_t rows, int64_t N, hipStream_t s)
+{
+    layer_realign<<<pass_grid(rows, (N + 7) / 8), dim3(kPassThreads), 0, s>>>(static_cast<const uint16_t*>(src), lds, static_cast<uint16_t*>(dst), ldd, rows, N);
+    return hipGetLastError();
 }
 
 hipError_t launch_epilogue(int64_t m, int64_t N, const EpilogueArgs& e, hipStream_t s)
