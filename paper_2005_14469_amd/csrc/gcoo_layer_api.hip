@@ -98,8 +98,16 @@ int check_values(const gcoo::RowsView& A, const void* dZ, int64_t lddz, const vo
     return N > 0 && A.nnz > 0 && (!dZ || !B) ? GCOO_EINVAL : GCOO_OK;
 }
 
-// Where the tiles of a row begin, then the sums of the parts.
-size_t values_bytes(const gcoo::RowsView& A, const gcoo::ValuesPlan& p) { return aligned((size_t)p.starts * 4) + (p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0); }
+// Where the tiles of a row begin, then the sums of the parts, then a copy of B.
+struct ValuesWork { size_t part, copy, total; };
+ValuesWork values_work(const gcoo::RowsView& A, const gcoo::ValuesPlan& p)
+{
+    ValuesWork w;
+    w.part = aligned((size_t)p.starts * 4);
+    w.copy = w.part + (p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0);
+    w.total = w.copy + aligned((size_t)A.k * (size_t)p.ldw * 2);
+    return w;
+}
 
 }  // namespace
 
@@ -110,7 +118,7 @@ size_t gcoo_spdm_grad_values_bytes(const gcoo_matrix* A, const void* dZ_dev, int
     if (!A) return 0;
     const gcoo::RowsView v = gcoo::rows_view(A);
     if (check_values(v, dZ_dev, lddz, B_dev, ldb, N, type) != GCOO_OK || v.nnz == 0) return 0;
-    return values_bytes(v, gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb));
+    return values_work(v, gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb)).total;
 }
 
 int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type,
@@ -123,11 +131,12 @@ int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz
     if (!on_floats(dvals_dev) || (v.nnz > 0 && !dvals_dev)) return GCOO_EINVAL;
     if (v.nnz == 0) return GCOO_OK;
     const gcoo::ValuesPlan plan = gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb);
-    rc = check_work(work, work_bytes, values_bytes(v, plan));
+    const ValuesWork w = values_work(v, plan);
+    rc = check_work(work, work_bytes, w.total);
     if (rc != GCOO_OK) return rc;
     const gcoo::GradValuesArgs a{v, dZ_dev, lddz, B_dev, ldb, N, type, dvals_dev};
-    float* part = reinterpret_cast<float*>(static_cast<char*>(work) + aligned((size_t)plan.starts * 4));
-    return done(gcoo::launch_grad_values(a, plan, static_cast<int32_t*>(work), part, static_cast<hipStream_t>(stream)), "gradient of the values");
+    char* at = static_cast<char*>(work);
+    return done(gcoo::launch_grad_values(a, plan, static_cast<int32_t*>(work), reinterpret_cast<float*>(at + w.part), at + w.copy, static_cast<hipStream_t>(stream)), "gradient of the values");
 }
 
 }  // extern "C"

@@ -27,9 +27,10 @@ struct ValuesPlan {
     bool one;              // a wave has one row of A, not four
     bool any;              // B by addresses in 64 bits
     int64_t starts;        // kValuesTiles: words for where the tiles of a row begin
+    int64_t ldw;           // not 0: B is copied first, to rows that many elements apart
 };
 ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb);
-// starts: plan.starts words; part: parts x nnz sums where there is more than one part
-hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, hipStream_t s);
+// starts: plan.starts words; part: parts x nnz sums where there is more than one part; copy: k x ldw elements of 2 bytes where ldw is not 0
+hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, void* copy, hipStream_t s);
 
 }  // namespace gcoo

@@ -573,11 +573,15 @@ static double tiles_time(double m, double k, double nnz, double N, int type)
 ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb)
 {
     const int64_t size = (int64_t)type_bytes(type), bytes = N * size;
-    ValuesPlan p{kValuesFew, 1, 1, false, false, 0};
+    ValuesPlan p{kValuesFew, 1, 1, false, false, 0, 0};
     if (bytes <= 64) return p;
     // (buffer loads at multiples of 4 bytes only)
     p.any = (uint64_t)k * (uint64_t)ldb * (uint64_t)size > kRowsMaxBytes || reinterpret_cast<uintptr_t>(B) % 4 != 0 || ldb * size % 4 != 0 || bytes % 4 != 0;
-    if (tiles_time((double)m, (double)k, (double)nnz, (double)N, type) < entries_time((double)nnz, (double)(m + k), (double)bytes, p.any && size == 2)) {
+    // (rows of 2-byte elements at odd places: as they are, or copied first)
+    const bool odd = odd_rows(B, ldb, type);
+    const double as_is = entries_time((double)nnz, (double)(m + k), (double)bytes, odd), copied = entries_time((double)nnz, (double)(m + k), (double)bytes, false) + 2.0 + 4.0 * (double)k * (double)N / 4.5e6;
+    const bool copies = odd && copied < as_is;
+    if (tiles_time((double)m, (double)k, (double)nnz, (double)N, type) < (copies ? copied : as_is)) {
         // tiles of 256 x 256 where they fill the compute units, else of 128 x 128 and as many parts of N as fill them twice, of four steps and more
         p.kernel = kValuesTiles;
         p.pieces = type != GCOO_F32 && ((m + 255) / 256) * ((k + 255) / 256) >= 160 ? 4 : 2;
@@ -590,6 +594,10 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
     // The widest tile of B of which an XCD's L2 keeps all rows (us, 1, 2 and 4 pieces: bf16, 0.5 %: 2000 x 2000, N = 4000: 24.6 22.6 22.1; 4000 x 4000, N = 4000: 53.0 48.6 47.4; 8000 x 8000, N = 8000:
     // 319 297 379; 14000 x 14000, N = 2000: 287 342 398; fp32: 4000 x 4000, N = 4000: 82 70 76; 8000 x 8000, N = 8000: 581 563 778), and one tile where N allows it.
     p.kernel = kValuesEntries;
+    if (copies) {
+        p.ldw = (N + 63) / 64 * 64;
+        p.any = (uint64_t)k * (uint64_t)p.ldw * 2u > kRowsMaxBytes || bytes % 4 != 0;
+    }
     if (bytes <= 1024) p.pieces = bytes <= 256 ? 1 : (bytes <= 512 ? 2 : 4);
     else p.pieces = k <= 3500 ? 4 : (k <= 10000 ? 2 : 1);
     p.parts = (int32_t)((bytes + 256 * p.pieces - 1) / (256 * p.pieces));
@@ -597,9 +605,17 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
     return p;
 }
 
-hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, hipStream_t s)
+hipError_t launch_grad_values(const GradValuesArgs& args, const ValuesPlan& plan, int32_t* starts, float* part, void* copy, hipStream_t s)
 {
-    hipError_t e = with_type(a.type, [&](auto t) {
+    GradValuesArgs a = args;
+    hipError_t e = hipSuccess;
+    if (plan.ldw > 0) {
+        e = launch_realign(a.B, a.ldb, copy, plan.ldw, a.A.k, a.N, s);
+        if (e != hipSuccess) return e;
+        a.B = copy;
+        a.ldb = plan.ldw;
+    }
+    e = with_type(a.type, [&](auto t) {
         typedef decltype(t) T;
         if (plan.kernel == kValuesFew) return launch_few<T>(a, s);
         if (plan.kernel == kValuesTiles) {

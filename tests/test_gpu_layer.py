@@ -106,6 +106,14 @@ def test_activations(act, dtype):
     forward_case(120, 80, 40, 0.3, "uniform", TYPES[dtype], act, True, False, True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("m,k,N,extra,shift,density", [(1500, 1600, 515, 0, 0, 0.05), (1500, 1600, 515, 5, 0, 0.05), (1500, 1600, 514, 0, 1, 0.02), (3000, 3000, 301, 0, 0, 0.02), (900, 1000, 17, 1, 0, 0.02), (700, 20000, 303, 0, 0, 0.01)])
+def test_rows_at_odd_places(m, k, N, extra, shift, density, dtype):
+    """An odd number of columns, odd leading dimensions and odd beginnings, where it pays to copy B first and where it does not."""
+    forward_case(m, k, N, density, "uniform", TYPES[dtype], "relu", True, True, True, extra, shift)
+    values_case(m, k, N, density, "uniform", TYPES[dtype], extra, shift)
+
+
 # the kernels that a product of this size and density takes: tiles of B in LDS, the sixteen-wave kernel in both cuts (also with uneven rows), rows of several tiles
 LARGE = [(1000, 900, 333, 0.05, "uniform", 32), (2000, 1999, 1024, 0.1, "uniform", 32), (2000, 2500, 600, 0.15, "uniform", 32), (2600, 2600, 2600, 0.04, "uniform", 32),
          (3000, 3001, 1000, 0.06, "zipf", 32), (2600, 2600, 520, 0.02, "uniform", 128), (6000, 500, 40, 0.02, "uniform", 8), (20000, 300, 12, 0.01, "uniform", 32)]
