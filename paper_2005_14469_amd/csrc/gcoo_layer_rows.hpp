@@ -111,8 +111,10 @@ hipError_t launch_layer_rows_ahead(const RowsArgs& a, const EpilogueArgs& e, int
 template <typename T, int LPR, int SUMS = LPR <= 16 ? 1 : LPR / 16>
 hipError_t launch_layer_rows(const RowsArgs& a, const EpilogueArgs& e, int64_t N4, hipStream_t s)
 {
+    // (2-byte elements up to 24 entries per row, whose waves have more registers to lose; us, sixteen and eight rows of B on their way: 4000 x 4000, rows of 20, N = 4000: bf16 55.4 47.3, fp16 47.7 41.3; 14000 x 14000, of 28,
+    // N = 2000: 125 137.  By matrix instructions, each value as three numbers in bf16, rows of 40 took as long: the caches are the bound)
     if constexpr (LPR >= 16)
-        if (a.nnz <= 16 * a.m) return launch_layer_rows_ahead<T, LPR, false, 8, SUMS>(a, e, N4, s);
+        if (a.nnz <= (sizeof(T) == 2 ? 24 : 16) * a.m) return launch_layer_rows_ahead<T, LPR, false, 8, SUMS>(a, e, N4, s);
     return launch_layer_rows_ahead<T, LPR, false, 16, SUMS>(a, e, N4, s);
 }
 

@@ -107,6 +107,23 @@ def refusals():
     assert 0 < need and H.clip(t, bytes=need - 1) == ENOMEM and not H.launches()
 
 
+def kernels():
+    """The shapes of layer_reference.KERNELS launch the kernels that they are there for."""
+    from tests import layer_reference as ref
+    from paper_2005_14469_amd import workloads
+    H = Layer()
+    types = {"f32": F32, "bf16": BF16, "f16": F16}
+    for shapes, call in ((ref.KERNELS, "forward"), (ref.VALUES_KERNELS, "values")):
+        for (m, k, N, density, kind, dtypes), name in shapes:
+            nnz = len(workloads.zipf_rows(m, k, 1, m + N, row_max=min(k, 3000)).vals) if kind == "zipf" else int(density * m * k * (2 / 3 if kind == "loose" else 1) + (64 * 0.9 * k if kind == "heavy" else 0))
+            h = H.matrix(m, k, nnz, 32)
+            for dtype in dtypes.split():
+                H.log()
+                rc = H.forward(h, N=N, type=types[dtype]) if call == "forward" else H.values(h, N=N, lddz=N, ldb=N, type=types[dtype])
+                launched = H.launches()
+                assert rc == OK and any(name.format(ref.MANGLED[dtype]) in x for x in launched), ((m, k, N, density, kind, dtype), name, launched)
+
+
 def a_launch_that_fails():
     H = Layer()
     h = H.matrix(30, 40, 200, 32)
@@ -126,5 +143,5 @@ def launches_of_clipping():
 
 
 if __name__ == "__main__":
-    {f.__name__: f for f in (refusals, a_launch_that_fails, launches_of_clipping)}[sys.argv[1]]()
+    {f.__name__: f for f in (refusals, kernels, a_launch_that_fails, launches_of_clipping)}[sys.argv[1]]()
     print("ok")

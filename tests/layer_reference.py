@@ -48,6 +48,24 @@ def slope(name, z):
     return np.ones_like(z)
 
 
+# ("heavy": 64 rows almost full, the others with as many entries as the density says)
+# Products and gradients of sizes at which every kernel that the library chooses among runs: (m, k, N, density, kind, types), and a part of the name of the kernel (its launches are checked without a GPU, its results on one).
+# Forward
+KERNELS = [((4000, 4000, 4000, 0.05, "uniform", "f32 bf16 f16"), "layer_bandI{}Li4ELb0ELb1E"), ((6000, 6000, 6001, 0.02, "uniform", "f32 bf16 f16"), "layer_bandI{}Li4ELb0ELb0E"), ((6000, 6000, 6000, 0.01, "uniform", "f32"), "layer_bandI{}Li2"),
+           ((9000, 9000, 9000, 0.0057, "zipf", "f32"), "layer_rows_allI{}"), ((6000, 6000, 6000, 0.02, "heavy", "f32 bf16 f16"), "layer_rows_allI{}"), ((6000, 6000, 5001, 0.02, "heavy", "f32 bf16 f16"), "layer_rows_allI{}"),
+           ((4500, 4500, 2000, 0.003, "uniform", "bf16 f16"), "layer_rowsI{}Li32ELb0ELi8E"), ((4500, 4500, 2000, 0.008, "uniform", "bf16 f16"), "layer_rowsI{}Li32ELb0ELi16E"), ((5500, 5500, 2000, 0.006, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb0ELi16E"),
+           ((4500, 4500, 2001, 0.003, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb1E"), ((8000, 8000, 40, 0.002, "uniform", "bf16 f16"), "layer_rowsI{}Li8E"), ((8000, 8000, 21, 0.002, "uniform", "f32"), "layer_rowsI{}Li8E"),
+           ((17000, 5000, 22, 0.002, "uniform", "bf16 f16"), "layer_rowsI{}Li4E"), ((5000, 5000, 1000, 0.004, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb0ELi8E"), ((3000, 9000, 300, 0.02, "zipf", "bf16 f16"), "layer_rowsI{}"),
+           ((3000, 9000, 301, 0.02, "heavy", "f32 bf16 f16"), "layer_rowsI{}"),
+           ((3000, 4000, 1, 0.2, "uniform", "f32 bf16 f16"), "layer_fewI{}Li64ELi1ELi4ELb1"), ((3000, 3001, 3, 0.15, "loose", "f32 bf16 f16"), "layer_fewI{}Li64ELi4ELi2ELb1"), ((3000, 3001, 7, 0.1, "loose", "bf16 f16"), "layer_fewI{}Li64ELi8ELi1ELb1"),
+           ((30000, 800, 2, 0.1, "loose", "f32 bf16 f16"), "layer_fewI{}Li16ELi4ELi2ELb1"), ((2000, 1900, 1001, 0.05, "uniform", "f32 bf16 f16"), "layer_tileI{}")]
+# the gradient of the stored weights
+VALUES_KERNELS = [((4000, 3900, 300, 0.2, "uniform", "bf16 f16"), "values_tilesI{}Li2ELi4ELi4"), ((3600, 4100, 513, 0.1, "loose", "bf16 f16"), "values_tilesI{}Li2ELi4ELi4"), ((1100, 1030, 1500, 0.4, "loose", "f32 bf16 f16"), "values_tilesI{}Li2ELi2ELi2"),
+                  ((1000, 12000, 1500, 0.003, "uniform", "f32 bf16 f16"), "values_entriesI{}Li1E"), ((3000, 5000, 2001, 0.004, "zipf", "f32 bf16 f16"), "values_entriesI{}Li2E"), ((3000, 3000, 1200, 0.004, "zipf", "f32 bf16 f16"), "values_entriesI{}Li4E"),
+                  ((9000, 3000, 24, 0.01, "loose", "f32 bf16 f16"), "values_"), ((3000, 3000, 1200, 0.01, "heavy", "f32 bf16 f16"), "values_entriesI{}Li4E"), ((5000, 4000, 2001, 0.01, "uniform", "bf16 f16"), "layer_realign")]
+MANGLED = {"f32": "f", "bf16": "DF16b", "f16": "DF16_"}
+
+
 def f64(t):
     return None if t is None else t.detach().double().cpu().numpy()
 
@@ -100,3 +118,11 @@ def check(got, want, off, what=""):
     assert np.array_equal(got[~finite & ~np.isnan(want)], want[~finite & ~np.isnan(want)]), what
     bad = np.abs(got[finite] - want[finite]) > off[finite]
     assert not bad.any(), (what, int(bad.sum()), float((np.abs(got - want)[finite] / np.maximum(off[finite], 1e-300)).max()))
+
+
+def check_on_gpu(got, want, off, what=""):
+    """check() where both are on the GPU in 64 bits."""
+    got = got.double()
+    assert got.shape == want.shape, what
+    bad = (got - want).abs() > off
+    assert not bad.any() and torch.isfinite(got).all(), (what, int(bad.sum()), float(((got - want).abs() / off.clamp(min=1e-300)).max()))

@@ -14,14 +14,23 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
 
 def csr(m, k, density, seed, kind="uniform"):
-    """row_ptr, cols, vals: "uniform", "zipf" (rows of very different lengths), "loose" (columns in no order, some twice, every third row empty)"""
+    """row_ptr, cols, vals: "uniform", "zipf" (rows of very different lengths), "loose" (columns in no order, some twice, every third row empty),
+    "heavy" (64 rows from row 700 on almost full)"""
     if kind == "zipf":
         w = workloads.zipf_rows(m, k, 1, seed, row_max=min(k, 3000))
         return w.row_ptr, w.col_idx, w.vals
+    rng = np.random.default_rng(seed)
+    if kind == "heavy":
+        mask = rng.random((m, k), dtype=np.float32) < density
+        mask[700:764] = rng.random((64, k), dtype=np.float32) < 0.9
+        cells = np.flatnonzero(mask)
+        return workloads.csr_from_cells(m, k, cells, rng.standard_normal(len(cells)).astype(np.float32))
+    if kind == "uniform" and m * k > 4000000:
+        cells = np.flatnonzero(rng.random((m, k), dtype=np.float32) < density)
+        return workloads.csr_from_cells(m, k, cells, rng.standard_normal(len(cells)).astype(np.float32))
     w = workloads.uniform_random(m, k, 1, 1 - density, seed)
     if kind == "uniform":
         return w.row_ptr, w.col_idx, w.vals
-    rng = np.random.default_rng(seed)
     lens = rng.integers(0, max(2, int(2 * density * k)), size=m)
     lens[::3] = 0
     row_ptr = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
@@ -114,13 +123,58 @@ def test_rows_at_odd_places(m, k, N, extra, shift, density, dtype):
     values_case(m, k, N, density, "uniform", TYPES[dtype], extra, shift)
 
 
-# the kernels that a product of this size and density takes: tiles of B in LDS, the sixteen-wave kernel in both cuts (also with uneven rows), rows of several tiles
-LARGE = [(1000, 900, 333, 0.05, "uniform", 32), (2000, 1999, 1024, 0.1, "uniform", 32), (2000, 2500, 600, 0.15, "uniform", 32), (2600, 2600, 2600, 0.04, "uniform", 32),
-         (3000, 3001, 1000, 0.06, "zipf", 32), (2600, 2600, 520, 0.02, "uniform", 128), (6000, 500, 40, 0.02, "uniform", 8), (20000, 300, 12, 0.01, "uniform", 32)]
+def every(list_):
+    return [(*shape[:5], dtype) for shape, _ in list_ for dtype in shape[5].split()]
+
+
+@pytest.mark.parametrize("m,k,N,density,kind,dtype", every(ref.KERNELS))
+def test_forward_by_every_kernel(m, k, N, density, kind, dtype):
+    """Against products of dense matrices in 64 bits."""
+    T = TYPES[dtype]
+    print(f"forward: {m} x {k} x {N} {density} {kind} {dtype}", flush=True)
+    arrays = csr(m, k, density, m + N, kind)
+    A = matrix(m, k, arrays)
+    rows = torch.from_numpy(np.repeat(np.arange(m), np.diff(arrays[0]))).to(DEV)
+    W = torch.zeros((m, k), dtype=torch.float64, device=DEV)
+    W.index_put_((rows, torch.from_numpy(arrays[1]).to(DEV).long()), torch.from_numpy(arrays[2]).to(DEV).double(), accumulate=True)
+    M = torch.zeros_like(W)
+    M.index_put_((rows, torch.from_numpy(arrays[1]).to(DEV).long()), torch.from_numpy(arrays[2]).to(DEV).double().abs(), accumulate=True)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(m + k)
+    B, R = torch.randn((k, N), generator=gen, device=DEV).to(T), torch.randn((m, N), generator=gen, device=DEV).to(T)
+    b = torch.randn(m, generator=gen, device=DEV)
+    C, Z = torch.full((m, N + 1), 7.0, dtype=T, device=DEV), torch.full((m, N + 3), 7.0, dtype=T, device=DEV)
+    binding.gcoo_spdm_epilogue(A, B, bias=b, activation="relu", residual=R, C_out=C[:, :N], Z_out=Z[:, :N])
+    z = W @ B.double() + b.double()[:, None]
+    off = (torch.from_numpy(np.diff(arrays[0])).to(DEV).double()[:, None] + 2) * ref.F32 * (M @ B.double().abs()) + ref.F32 * z.abs()
+    u, least = ref.U[T], ref.LEAST[T]
+    ref.check_on_gpu(Z[:, :N], z, off + u * (z.abs() + off) + least, "Z")
+    y = z.clamp(min=0) + R.double()
+    off = off + ref.F32 * y.abs()
+    ref.check_on_gpu(C[:, :N], y, off + u * (y.abs() + off) + least, "C")
+    assert torch.all(C[:, N:] == 7.0) and torch.all(Z[:, N:] == 7.0)
+    again = binding.gcoo_spdm_epilogue(A, B, bias=b, activation="relu", residual=R)
+    assert torch.equal(again, C[:, :N])
+
+
+@pytest.mark.parametrize("m,k,N,density,kind,dtype", every(ref.VALUES_KERNELS))
+def test_grad_values_by_every_kernel(m, k, N, density, kind, dtype):
+    T = TYPES[dtype]
+    print(f"values: {m} x {k} x {N} {density} {kind} {dtype}", flush=True)
+    arrays = csr(m, k, density, m + N, kind)
+    A = matrix(m, k, arrays)
+    rows, cols = torch.from_numpy(np.repeat(np.arange(m), np.diff(arrays[0]))).to(DEV), torch.from_numpy(arrays[1]).to(DEV).long()
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(m + k)
+    dZ, B = torch.randn((m, N), generator=gen, device=DEV).to(T), torch.randn((k, N), generator=gen, device=DEV).to(T)
+    got = binding.gcoo_spdm_grad_values(A, dZ, B)
+    want, off = (dZ.double() @ B.double().t().contiguous())[rows, cols], (N + 2) * ref.F32 * (dZ.double().abs() @ B.double().abs().t().contiguous())[rows, cols]
+    ref.check_on_gpu(got, want, off, "dvals")
+    assert torch.equal(binding.gcoo_spdm_grad_values(A, dZ, B), got)
 
 
 @pytest.mark.parametrize("dtype", list(TYPES))
-@pytest.mark.parametrize("m,k,N,density,kind,p", LARGE)
+@pytest.mark.parametrize("m,k,N,density,kind,p", [(1000, 900, 333, 0.05, "uniform", 32), (2600, 2600, 520, 0.02, "uniform", 128), (6000, 500, 40, 0.02, "uniform", 8), (20000, 300, 12, 0.01, "uniform", 32), (1500, 2000, 100, 0.03, "zipf", 200)])
 def test_forward_large(m, k, N, density, kind, p, dtype):
     forward_case(m, k, N, density, kind, TYPES[dtype], "silu", True, True, True, p=p)
 

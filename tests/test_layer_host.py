@@ -12,7 +12,7 @@ def stub():
     host_calls.build()
 
 
-@pytest.mark.parametrize("case", ["refusals", "a_launch_that_fails", "launches_of_clipping"])
+@pytest.mark.parametrize("case", ["refusals", "kernels", "a_launch_that_fails", "launches_of_clipping"])
 def test_host_code(case):
     r = subprocess.run([sys.executable, "-m", "tests.layer_calls", case], cwd=host_calls.ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.endswith("ok\n"), r.stdout + r.stderr
