@@ -191,12 +191,13 @@ int check_clip_ranges(const gcoo_gradient* list, int64_t tensors, const float* n
 
 // How many launches the tensors are, and how many workgroups each has at the most.
 struct ClipLaunches { int64_t launches, wgs; };
-ClipLaunches clip_launches(const gcoo_gradient* list, int64_t tensors)
+ClipLaunches clip_launches(const gcoo_gradient* list, int64_t tensors, int64_t pieces)
 {
     int64_t full = 0;
     for (int64_t i = 0; i < tensors; ++i) full += list[i].count > 0;
     const int64_t launches = (full + gcoo::kClipTensors - 1) / gcoo::kClipTensors;
-    return {launches, launches > 0 ? std::max<int64_t>(gcoo::kClipSums / launches, 64) : 0};
+    if (launches <= 1 && pieces <= gcoo::kClipSmallPieces) return {1, 0};                       // by one workgroup
+    return {launches, std::max<int64_t>(gcoo::kClipSums / launches, 64)};
 }
 // f(list of a launch) for the tensors, as many as a launch takes at a time.
 template <typename F>
@@ -224,8 +225,9 @@ extern "C" {
 
 size_t gcoo_clip_grad_norm_bytes(const gcoo_gradient* list, int64_t tensors)
 {
-    if (check_clip(list, tensors) <= 0) return 0;
-    const ClipLaunches n = clip_launches(list, tensors);
+    const int64_t pieces = check_clip(list, tensors);
+    if (pieces <= 0) return 0;
+    const ClipLaunches n = clip_launches(list, tensors, pieces);
     return aligned((size_t)(n.launches * n.wgs) * sizeof(double));
 }
 
@@ -239,8 +241,9 @@ int gcoo_clip_grad_norm(const gcoo_gradient* list, int64_t tensors, float max_no
     if (rc != GCOO_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     double* sums = static_cast<double*>(work);
-    if (pieces == 0) return done(gcoo::launch_clip_scale(gcoo::ClipList{}, nullptr, 0, max_norm, norm_dev, s), "clip_scale launch");
-    const int64_t most = clip_launches(list, tensors).wgs;
+    if (pieces == 0) return done(gcoo::launch_clip_small(gcoo::ClipList{}, max_norm, norm_dev, s), "clip_small launch");
+    const int64_t most = clip_launches(list, tensors, pieces).wgs;
+    if (most == 0) return each_clip_launch(list, tensors, 0, [&](const gcoo::ClipList& l) { return done(gcoo::launch_clip_small(l, max_norm, norm_dev, s), "clip_small launch"); });
     int32_t sums_all = 0;
     rc = each_clip_launch(list, tensors, most, [&](const gcoo::ClipList& l) {
         sums_all = l.sum0 + l.wgs;

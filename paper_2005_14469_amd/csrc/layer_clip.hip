@@ -22,13 +22,10 @@ __device__ __forceinline__ int clip_tensor(const ClipList& l, int32_t piece)
     return lo;
 }
 
-// f(tensor, first element, elements) for the pieces of the workgroup; DOWN: from the last to the first, the workgroups too.
+// f(tensor, first element, elements) for the pieces [from, to); DOWN: from the last to the first.
 template <bool DOWN, typename F>
-__device__ __forceinline__ void clip_pieces(const ClipList& l, F&& f)
+__device__ __forceinline__ void clip_stretch(const ClipList& l, int32_t from, int32_t to, F&& f)
 {
-    if (l.pieces == 0) return;
-    const int32_t wg = DOWN ? l.wgs - 1 - (int32_t)blockIdx.x : (int32_t)blockIdx.x;
-    const int32_t from = (int32_t)((int64_t)l.pieces * wg / l.wgs), to = (int32_t)((int64_t)l.pieces * (wg + 1) / l.wgs);
     if (from >= to) return;
     int x = clip_tensor(l, DOWN ? to - 1 : from);
     for (int32_t i = 0; i < to - from; ++i) {
@@ -40,30 +37,47 @@ __device__ __forceinline__ void clip_pieces(const ClipList& l, F&& f)
     }
 }
 
-template <typename T> constexpr int kClipVec = 16 / sizeof(T);
-template <typename T> constexpr int kClipSteps = kClipPiece / (kClipThreads * kClipVec<T>);       // 16-byte pieces of a thread
+// the same for the pieces of the workgroup; DOWN: the workgroups from the last to the first, too
+template <bool DOWN, typename F>
+__device__ __forceinline__ void clip_pieces(const ClipList& l, F&& f)
+{
+    const int32_t wg = DOWN ? l.wgs - 1 - (int32_t)blockIdx.x : (int32_t)blockIdx.x;
+    clip_stretch<DOWN>(l, (int32_t)((int64_t)l.pieces * wg / l.wgs), (int32_t)((int64_t)l.pieces * (wg + 1) / l.wgs), f);
+}
 
-template <typename T>
-__device__ __forceinline__ double clip_squares(const T* x, int n)
+template <typename T> constexpr int kClipVec = 16 / sizeof(T);
+template <typename T, int THREADS> constexpr int kClipSteps = kClipPiece / (THREADS * kClipVec<T>);       // 16-byte pieces of a thread
+
+// `t`: the thread's place among THREADS of them
+template <int THREADS, typename T>
+__device__ __forceinline__ double clip_squares(const T* x, int n, int t)
 {
     constexpr int V = kClipVec<T>;
     double sum = 0.0;
-    float v[kClipSteps<T>][V];
+    float v[kClipSteps<T, THREADS>][V];
 #pragma unroll
-    for (int s = 0; s < kClipSteps<T>; ++s) {
-        const int at = (s * kClipThreads + (int)threadIdx.x) * V;
+    for (int s = 0; s < kClipSteps<T, THREADS>; ++s) {
+        const int at = (s * THREADS + t) * V;
         if (at + V <= n) layer_load<T, V>(x, at, v[s]);
         else
 #pragma unroll
             for (int u = 0; u < V; ++u) v[s][u] = at + u < n ? widen(x[at + u]) : 0.0f;
     }
 #pragma unroll
-    for (int s = 0; s < kClipSteps<T>; ++s)
+    for (int s = 0; s < kClipSteps<T, THREADS>; ++s)
 #pragma unroll
         for (int u = 0; u < V; ++u) sum = __builtin_fma((double)v[s][u], (double)v[s][u], sum);
     return sum;
 }
+template <int THREADS>
+__device__ __forceinline__ double clip_squares_of(const ClipTensor& t, int64_t at, int n, int thread)
+{
+    if (t.type == GCOO_F32) return clip_squares<THREADS>(static_cast<const float*>(t.data) + at, n, thread);
+    if (t.type == GCOO_BF16) return clip_squares<THREADS>(static_cast<const bf16_t*>(t.data) + at, n, thread);
+    return clip_squares<THREADS>(static_cast<const f16_t*>(t.data) + at, n, thread);
+}
 
+template <int WAVES>
 __device__ __forceinline__ double clip_block_sum(double sum, double* part)
 {
 #pragma unroll
@@ -71,7 +85,7 @@ __device__ __forceinline__ double clip_block_sum(double sum, double* part)
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     sum = 0.0;
-    for (int w = 0; w < kClipThreads / 64; ++w) sum += part[w];
+    for (int w = 0; w < WAVES; ++w) sum += part[w];
     return sum;
 }
 
@@ -79,34 +93,30 @@ __global__ __launch_bounds__(kClipThreads) void clip_sum(ClipList l, double* sum
 {
     __shared__ double part[kClipThreads / 64];
     double sum = 0.0;
-    clip_pieces<false>(l, [&](const ClipTensor& t, int64_t at, int n) {
-        if (t.type == GCOO_F32) sum += clip_squares(static_cast<const float*>(t.data) + at, n);
-        else if (t.type == GCOO_BF16) sum += clip_squares(static_cast<const bf16_t*>(t.data) + at, n);
-        else sum += clip_squares(static_cast<const f16_t*>(t.data) + at, n);
-    });
-    sum = clip_block_sum(sum, part);
+    clip_pieces<false>(l, [&](const ClipTensor& t, int64_t at, int n) { sum += clip_squares_of<kClipThreads>(t, at, n, (int)threadIdx.x); });
+    sum = clip_block_sum<kClipThreads / 64>(sum, part);
     if (threadIdx.x == 0) sums[l.sum0 + (int32_t)blockIdx.x] = sum;
 }
 
 // (x may be y: a thread loads what it stores itself)
-template <typename T>
-__device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t first, int n, float factor)
+template <int THREADS, typename T>
+__device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t first, int n, float factor, int t)
 {
     constexpr int V = kClipVec<T>;
     const T* x = static_cast<const T*>(data) + first;
     T* y = static_cast<T*>(out) + first;
-    float v[kClipSteps<T>][V];
+    float v[kClipSteps<T, THREADS>][V];
 #pragma unroll
-    for (int s = 0; s < kClipSteps<T>; ++s) {
-        const int at = (s * kClipThreads + (int)threadIdx.x) * V;
+    for (int s = 0; s < kClipSteps<T, THREADS>; ++s) {
+        const int at = (s * THREADS + t) * V;
         if (at + V <= n) layer_load<T, V>(x, at, v[s]);
         else
 #pragma unroll
             for (int u = 0; u < V; ++u) v[s][u] = at + u < n ? widen(x[at + u]) : 0.0f;
     }
 #pragma unroll
-    for (int s = 0; s < kClipSteps<T>; ++s) {
-        const int at = (s * kClipThreads + (int)threadIdx.x) * V;
+    for (int s = 0; s < kClipSteps<T, THREADS>; ++s) {
+        const int at = (s * THREADS + t) * V;
 #pragma unroll
         for (int u = 0; u < V; ++u) v[s][u] *= factor;
         if (at + V <= n) layer_store<T, V>(y, at, v[s]);
@@ -117,23 +127,56 @@ __device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t
     }
 }
 
+// What the norm of all says is to be done.
+struct ClipFactor {
+    bool scales;
+    float f;
+    __device__ __forceinline__ ClipFactor(float norm, float max_norm)
+    {
+        scales = !(max_norm >= norm + 1e-6f);                       // (a NaN scales)
+        f = scales ? max_norm / (norm + 1e-6f) : 1.0f;
+    }
+    template <int THREADS>
+    __device__ __forceinline__ void apply(const ClipTensor& t, int64_t at, int n, int thread) const
+    {
+        if (!scales && t.data == t.out) return;
+        if (t.type == GCOO_F32) clip_scaled<THREADS, float>(t.data, t.out, at, n, f, thread);
+        else if (t.type == GCOO_BF16) clip_scaled<THREADS, bf16_t>(t.data, t.out, at, n, f, thread);
+        else clip_scaled<THREADS, f16_t>(t.data, t.out, at, n, f, thread);
+    }
+};
+
 __global__ __launch_bounds__(kClipThreads) void clip_scale(ClipList l, const double* sums, int32_t sums_all, float max_norm, float* norm_out)
 {
     __shared__ double part[kClipThreads / 64];
     double sum = 0.0;
     for (int32_t i = threadIdx.x; i < sums_all; i += kClipThreads) sum += sums[i];
-    const float norm = (float)sqrt(clip_block_sum(sum, part));
+    const float norm = (float)sqrt(clip_block_sum<kClipThreads / 64>(sum, part));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-    const bool scales = !(max_norm >= norm + 1e-6f);                // (a NaN scales)
-    const float f = scales ? max_norm / (norm + 1e-6f) : 1.0f;
-    clip_pieces<true>(l, [&](const ClipTensor& t, int64_t at, int n) {
-        if (!scales && t.data == t.out) return;
-        if (t.type == GCOO_F32) clip_scaled<float>(t.data, t.out, at, n, f);
-        else if (t.type == GCOO_BF16) clip_scaled<bf16_t>(t.data, t.out, at, n, f);
-        else clip_scaled<f16_t>(t.data, t.out, at, n, f);
-    });
+    const ClipFactor factor(norm, max_norm);
+    clip_pieces<true>(l, [&](const ClipTensor& t, int64_t at, int n) { factor.apply<kClipThreads>(t, at, n, (int)threadIdx.x); });
 }
 
+// A few pieces: one workgroup, whose quarters take a stretch each, and one launch (us, two launches and so, fp32: 2000 elements: 7.3 5.5; 16384: 6.6 5.4; 24576: 6.7 6.5; 49152: 6.9 9.3).
+__global__ __launch_bounds__(kClipSmallThreads) void clip_small(ClipList l, float max_norm, float* norm_out)
+{
+    __shared__ double part[kClipSmallThreads / 64];
+    constexpr int GROUPS = kClipSmallThreads / kClipThreads;
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / kClipThreads), t = (int)threadIdx.x % kClipThreads;
+    const int32_t from = l.pieces * group / GROUPS, to = l.pieces * (group + 1) / GROUPS;
+    double sum = 0.0;
+    clip_stretch<false>(l, from, to, [&](const ClipTensor& x, int64_t at, int n) { sum += clip_squares_of<kClipThreads>(x, at, n, t); });
+    const float norm = (float)sqrt(clip_block_sum<kClipSmallThreads / 64>(sum, part));
+    if (threadIdx.x == 0) *norm_out = norm;
+    const ClipFactor factor(norm, max_norm);
+    clip_stretch<true>(l, from, to, [&](const ClipTensor& x, int64_t at, int n) { factor.apply<kClipThreads>(x, at, n, t); });
+}
+
+hipError_t launch_clip_small(const ClipList& l, float max_norm, float* norm_out, hipStream_t s)
+{
+    clip_small<<<dim3(1), dim3(kClipSmallThreads), 0, s>>>(l, max_norm, norm_out);
+    return hipGetLastError();
+}
 hipError_t launch_clip_sum(const ClipList& l, double* sums, hipStream_t s)
 {
     clip_sum<<<dim3((unsigned)l.wgs), dim3(kClipThreads), 0, s>>>(l, sums);
@@ -141,8 +184,7 @@ hipError_t launch_clip_sum(const ClipList& l, double* sums, hipStream_t s)
 }
 hipError_t launch_clip_scale(const ClipList& l, const double* sums, int32_t sums_all, float max_norm, float* norm_out, hipStream_t s)
 {
-    // (a list without pieces: one workgroup that writes the norm)
-    clip_scale<<<dim3((unsigned)(l.wgs > 0 ? l.wgs : 1)), dim3(kClipThreads), 0, s>>>(l, sums, sums_all, max_norm, norm_out);
+    clip_scale<<<dim3((unsigned)l.wgs), dim3(kClipThreads), 0, s>>>(l, sums, sums_all, max_norm, norm_out);
     return hipGetLastError();
 }
 

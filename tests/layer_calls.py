@@ -93,18 +93,21 @@ def refusals():
     assert H.values(none, dZ=None, B=None, out=None) == OK and not H.launches()
 
     t = (AT, AT, 100, F32)
-    assert H.clip(t) == OK and len(H.launches()) == 2
+    assert H.clip(t) == OK and len(H.launches()) == 1
     for tensors in ([(AT, AT, -1, F32)], [(AT, AT, 10, 3)], [(None, AT, 10, F32)], [(AT, None, 10, F32)], [(AT + 2, AT + 2, 10, F32)], [(AT, AT + 1, 10, F16)], [t, t], [t, (AT + 396, AT + 396, 10, F32)],
                     [(AT, AT + 4, 100, F32)], [(AT, 2 * AT, 100, F32), (2 * AT + 8, 3 * AT, 10, F32)], [(AT, 2 * AT, 100, F32), (3 * AT, 2 * AT + 198, 10, BF16)], [(AT, AT, 1 << 61, F32)], [(AT, AT, 1 << 50, F32)]):
         H.refused(H.clip(*tensors), tensors)
-    for kw in (dict(norm=None), dict(norm=AT + 2), dict(norm=AT + 396), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(work=None)):
+    for kw in (dict(norm=None), dict(norm=AT + 2), dict(norm=AT + 396), dict(max_norm=-1.0), dict(max_norm=float("nan"))):
         H.refused(H.clip(t, **kw), kw)
     assert H.clip((AT, 2 * AT, 100, F32), (AT, 3 * AT, 100, F32), (AT + 400, AT + 400, 5, F32)) == OK and H.launches()      # (read twice, written once each)
     assert H.clip((None, None, 0, F32), max_norm=float("inf"), work=None, bytes=0) == OK and len(H.launches()) == 1
     assert H.clip(bytes=0, work=None) == OK and len(H.launches()) == 1
     H.refused(H.L.gcoo_clip_grad_norm(None, 1, 1.0, AT, AT, 1 << 50, None), "no list")
-    need = H.L.gcoo_clip_grad_norm_bytes((Gradient * 1)(Gradient(*t)), 1)
-    assert 0 < need and H.clip(t, bytes=need - 1) == ENOMEM and not H.launches()
+    many = (AT, AT, 1000000, F32)
+    need = H.L.gcoo_clip_grad_norm_bytes((Gradient * 1)(Gradient(*many)), 1)
+    assert 0 < need and H.clip(many, norm=AT - 4, bytes=need) == OK and len(H.launches()) == 2
+    assert H.clip(many, bytes=need - 1) == ENOMEM and not H.launches()
+    H.refused(H.clip(many, work=None), "no work")
 
 
 def kernels():
@@ -136,10 +139,12 @@ def a_launch_that_fails():
 def launches_of_clipping():
     """Many tensors are as many launches as their descriptions fill; the norm is written once."""
     H = Layer()
-    for n, launches in ((1, 2), (80, 2), (81, 4), (400, 10)):
+    for n, launches in ((1, 1), (6, 1), (7, 2), (80, 2), (81, 4), (400, 10)):
         assert H.clip(*[(AT + 4096 * i, AT + 4096 * i, 1 + i, F32) for i in range(n)]) == OK
         assert len(H.launches()) == launches, n
     assert H.clip(*[(AT + 4096 * i, AT + 4096 * i, i % 2, F32) for i in range(160)]) == OK and len(H.launches()) == 2
+    for count, launches in ((6 * 4096, 1), (6 * 4096 + 1, 2)):
+        assert H.clip((AT, AT, count, F32)) == OK and len(H.launches()) == launches
 
 
 if __name__ == "__main__":
