@@ -63,6 +63,8 @@ def parse():
                     help="instead of the headline run: the row-by-row kernel and the sixteen-wave kernel, which the automatic choice is between, against "
                          "the register kernel (p = 32, 38) and the workgroup-shared kernel (p = 32, 42, 48) on uniform random square matrices, "
                          "kernel and conversion times")
+    ap.add_argument("--layer", action="store_true",
+                    help="time a training step of a layer with the secondary workload's weights (forward with its epilogue, all gradients, clipping), bf16 and fp32")
     ap.add_argument("--copy-calibration", action="store_true",
                     help="only run a plain 256 MiB device copy a few times: the reference launch against which the "
                          "FETCH_SIZE / WRITE_SIZE counters of rocprofv3 --pmc are scaled")
@@ -419,6 +421,42 @@ def eo_kc(torch, binding, workloads, args, dev):
             "rows": rows}
 
 
+def layer(torch, binding, workloads, args, dev):
+    """A training step of C = gelu(A x B + bias) + residual, A the sparse weights: what the operators of a layer take one by one, and the step as a whole with new weights (both conversions in it)."""
+    rows = []
+    w = workloads.config(int(args.secondary[-1]))
+    m, k, N = w.m, w.k, w.N
+    rp, ci, va = [torch.from_numpy(x).to(dev) for x in (w.row_ptr, w.col_idx, w.vals)]
+    r = torch.repeat_interleave(torch.arange(m, device=dev, dtype=torch.int32), torch.diff(rp).long())
+    order = torch.argsort(ci.long() * m + r.long())
+    rpt = torch.zeros(k + 1, dtype=torch.int32, device=dev)
+    rpt[1:] = torch.cumsum(torch.bincount(ci, minlength=k), 0)
+    cit = r[order]
+    p, pt = binding.gcoo_default_p(m, k, w.nnz, N), binding.gcoo_default_p(k, m, w.nnz, N)
+    for dtype in (torch.bfloat16, torch.float32):
+        X, dY, R = (torch.randn((n, N), device=dev).to(dtype) for n in (k, m, m))
+        bias = torch.randn(m, device=dev)
+        Y, Z, dZ, dX = (torch.empty((n, N), device=dev, dtype=dtype) for n in (m, m, m, k))
+        held = {}
+
+        def convert():
+            held["A"] = binding.gcoo_from_csr(m, k, rp, ci, va, p, known_nnz=True)
+            held["At"] = binding.gcoo_from_csr(k, m, rpt, cit, va[order], pt, known_nnz=True)
+
+        calls = {"convert": convert,
+                 "forward": lambda: binding.gcoo_spdm_epilogue(held["A"], X, bias=bias, activation="gelu", residual=R, C_out=Y, Z_out=Z),
+                 "epilogue_grad": lambda: held.update(db=binding.gcoo_epilogue_grad(dY, Z=Z, activation="gelu", dZ_out=dZ)[1]),
+                 "grad_values": lambda: held.update(dv=binding.gcoo_spdm_grad_values(held["A"], dZ, X)),
+                 "grad_input": lambda: binding.gcoo_spdm_epilogue(held["At"], dZ, C_out=dX),
+                 "clip": lambda: held.update(norm=binding.gcoo_clip_grad_norm([held["dv"], held["db"]], 1.0))}
+        for call in calls.values():
+            call()
+        row = {"dtype": str(dtype).split(".")[1], **{name + "_ms": _event_ms(torch, call, 5) for name, call in calls.items()}}
+        row["step_ms"] = _event_ms(torch, lambda: [call() for call in calls.values()], 5)
+        rows.append(row)
+    return {"metric": "training step of a layer with sparse weights", "workload": f"{args.secondary}: A {m}x{k}, nnz={w.nnz}, N={N}", "rows": rows}
+
+
 def main():
     args = parse()
     if args.gpus != 1:
@@ -452,6 +490,9 @@ def main():
         return
     if args.kernels:
         print(json.dumps(kernels_compared(torch, binding, workloads, args, dev)))
+        return
+    if args.layer:
+        print(json.dumps(layer(torch, binding, workloads, args, dev)))
         return
     if args.sweep:
         print(json.dumps(sweep(torch, binding, workloads, args, dev)))
