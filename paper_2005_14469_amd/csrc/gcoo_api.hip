@@ -1795,7 +1795,8 @@ namespace gcoo {
 RowsView rows_view(const gcoo_matrix* A)
 {
     if (A->inner) A = A->inner;
-    return {A->m, A->k, A->nnz, A->row_start(), A->row_cols(), A->row_vals()};
+    const gcoo::RowsArgs r = rows_args(A, nullptr, 0, 0, nullptr, 0);
+    return {A->m, A->k, A->nnz, r.row_ptr, r.cols, r.vals, {r.long_rows, r.long_count, r.long_row, r.long_room}};
 }
 int hip_failed(hipError_t e, const char* what) { return hip_fail(e, what); }
 

@@ -9,12 +9,19 @@
 
 namespace gcoo {
 
+// The rows of more than long_row entries as the conversion lists them: the longest from the front, the others from the back (counted), or, without counts, in places of which some hold -1.
+struct LongRows {
+    const int32_t* rows;       // [room]
+    const int32_t* count;      // [0]: of those from the back, [2]: from the front; or null
+    int32_t long_row, room;
+};
 // The entries of a handle in row order.
 struct RowsView {
     int64_t m, k, nnz;
     const int32_t* start;      // [m + 1]
     const int32_t* cols;       // a device CSR input is not checked: whoever uses a column brings it below k
     const float* vals;
+    LongRows longs;
 };
 RowsView rows_view(const gcoo_matrix* A);
 int hip_failed(hipError_t e, const char* what);            // keeps the text for gcoo_last_hip_error()

@@ -5,6 +5,8 @@
 #include "gcoo_layer_device.hpp"
 #include "gcoo_spdm_rows_kernel.hpp"
 
+#include <type_traits>
+
 namespace gcoo {
 
 // COLS adjacent elements at any place.

@@ -2,6 +2,7 @@
 // columns; instances by type in layer_rows_*.hip.
 #pragma once
 #include "gcoo_layer_io.hpp"
+#include "gcoo_layer_long.hpp"
 
 namespace gcoo {
 
@@ -19,17 +20,23 @@ __global__ __launch_bounds__(kRowsThreads, AHEAD == 16 ? (LPR == 4 || (LPR == 16
 // Few columns: LANES lanes share a row, each takes four adjacent entries at a time with one load each of columns and values, GROUPS such on their way; their sums are added up in a fixed tree.
 // Bound for a single token: the entries, which are all that is read from memory.  The elements of B lie anywhere: from the vector cache a lane's takes a clock of its compute unit, so for many entries the whole
 // of B is brought to LDS first (HELD), which gives 64 lanes theirs in about five (8000 x 8000, 10 %, one token, bf16: 21 us from the cache, 13.4 so, of which reading the entries once at the rate of a large copy takes 10.4).
+// Long rows have workgroups of their own, `long_wgs` behind the others (us, one token: power-law rows, 16384 x 16384, of 53 entries, fp32: 28 10; ten full rows among 20000 of 20 entries: 113 14; with even rows level, but for two to seven
+// tokens on a held B: 8000 x 8000, 10 %, 3 tokens, bf16: 17.1 17.9).
 template <typename T, int LANES, int N, int GROUPS, bool HELD>
-__global__ __launch_bounds__(HELD ? kFewThreads : kRowsThreads) void layer_few(RowsArgs a, EpilogueArgs e)
+__global__ __launch_bounds__(HELD ? kFewThreads : kRowsThreads, HELD ? 8 : 1) void layer_few(RowsArgs a, EpilogueArgs e, int32_t long_wgs)
 {
-    constexpr int THREADS = HELD ? kFewThreads : kRowsThreads;
-    const int lane = threadIdx.x % LANES;
-    const int64_t r = (int64_t)blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
+    constexpr int THREADS = HELD ? kFewThreads : kRowsThreads, SLOTS = THREADS / LANES;
     const uint32_t kmax = (uint32_t)(a.k - 1);
     const T* B = reinterpret_cast<const T*>(a.B);
     const int n = (int)a.N;
     extern __shared__ __attribute__((aligned(16))) char few_smem[];
     T* held = reinterpret_cast<T*>(few_smem);                              // B, its rows one behind the other
+    const int32_t wgs = (int32_t)gridDim.x - long_wgs;
+    const bool shares = (int32_t)blockIdx.x >= wgs;
+    const LongRows longs{a.long_rows, shares ? a.long_count : nullptr, a.long_row, shares ? a.long_room : 0};
+    LongWalk<1> walk(longs, a.row_ptr, a.m, (int32_t)blockIdx.x - wgs, long_wgs);
+    int32_t long_row = 0, piece;
+    if (shares && !walk.next(&long_row, &piece)) return;
     if constexpr (HELD) {
         if (a.ldb == n) {
             // (the last bytes of B by elements)
@@ -48,53 +55,85 @@ __global__ __launch_bounds__(HELD ? kFewThreads : kRowsThreads) void layer_few(R
         }
         __syncthreads();
     }
-    if (r >= a.m) return;
-    float sum[N] = {};
-    const uint32_t end = (uint32_t)a.row_ptr[r + 1];                     // (unsigned: a step beyond the last of 2^31 entries stays a number)
+    const uint32_t lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     typedef uint32_t cols4 __attribute__((ext_vector_type(4), aligned(4)));
     typedef float vals4 __attribute__((ext_vector_type(4), aligned(4)));
-    for (uint32_t i = (uint32_t)a.row_ptr[r] + 4 * (uint32_t)lane; i < end; i += 4 * LANES * GROUPS) {
-        uint32_t c[GROUPS][4];
-        float v[GROUPS][4];
+    for (;;) {
+        // the row of these lanes, or a stretch of the workgroup's (unsigned: a step beyond the last of 2^31 entries stays a number)
+        int64_t r = (int64_t)blockIdx.x * SLOTS + slot;
+        uint32_t beg = 0, end = 0;
+        if (shares) {
+            r = long_row;
+            beg = (uint32_t)a.row_ptr[r];
+            end = (uint32_t)a.row_ptr[r + 1];
+            const uint32_t each = (end - beg + SLOTS - 1) / SLOTS;
+            beg += slot * each;
+            end = beg + each < end ? beg + each : end;
+        } else {
+            if (r >= a.m) return;
+            beg = (uint32_t)a.row_ptr[r];
+            end = (uint32_t)a.row_ptr[r + 1];
+            if ((int32_t)(end - beg) > a.long_row) return;
+        }
+        float sum[N] = {};
+        for (uint32_t i = beg + 4 * lane; i < end; i += 4 * LANES * GROUPS) {
+            uint32_t c[GROUPS][4];
+            float v[GROUPS][4];
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const uint32_t at = i + 4 * LANES * g;
-            if (at + 4 <= end) {
-                const cols4 x = *reinterpret_cast<const cols4*>(a.cols + at);
-                const vals4 y = *reinterpret_cast<const vals4*>(a.vals + at);
+            for (int g = 0; g < GROUPS; ++g) {
+                const uint32_t at = i + 4 * LANES * g;
+                if (at + 4 <= end) {
+                    const cols4 x = *reinterpret_cast<const cols4*>(a.cols + at);
+                    const vals4 y = *reinterpret_cast<const vals4*>(a.vals + at);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) { c[g][q] = x[q]; v[g][q] = y[q]; }
-            } else {
+                    for (int q = 0; q < 4; ++q) { c[g][q] = x[q]; v[g][q] = y[q]; }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const bool in = at + q < end;
+                        c[g][q] = in ? (uint32_t)a.cols[at + q] : 0u;
+                        v[g][q] = in ? a.vals[at + q] : 0.0f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const bool in = at + q < end;
-                    c[g][q] = in ? (uint32_t)a.cols[at + q] : 0u;
-                    v[g][q] = in ? a.vals[at + q] : 0.0f;
+                    const bool in = i + 4 * LANES * g + q < end;
+                    const uint32_t col = c[g][q] < kmax ? c[g][q] : kmax;
+                    const T* row = HELD ? held + col * (uint32_t)n : B + (int64_t)col * a.ldb;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float b = in && j < n ? widen(row[j]) : 0.0f;
+                        sum[j] = __builtin_fmaf(v[g][q], b, sum[j]);
+                    }
                 }
-            }
         }
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const bool in = i + 4 * LANES * g + q < end;
-                const uint32_t col = c[g][q] < kmax ? c[g][q] : kmax;
-                const T* row = HELD ? held + col * (uint32_t)n : B + (int64_t)col * a.ldb;
+            for (int d = LANES / 2; d >= 1; d >>= 1) sum[j] += __shfl_xor(sum[j], d, LANES);
+        bool stores = lane == 0;
+        if (shares) {
+            __shared__ float part[SLOTS][N];
+            if (lane == 0)
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float b = in && j < n ? widen(row[j]) : 0.0f;
-                    sum[j] = __builtin_fmaf(v[g][q], b, sum[j]);
-                }
-            }
-    }
+                for (int j = 0; j < N; ++j) part[slot][j] = sum[j];
+            __syncthreads();
+            stores = threadIdx.x == 0;
+            if (stores)
+                for (int w = 1; w < SLOTS; ++w)
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int d = LANES / 2; d >= 1; d >>= 1) sum[j] += __shfl_xor(sum[j], d, LANES);
-    if (lane == 0) {
-        float res[N];
-        layer_residual<T, N>(e, r, 0, 0, n, true, res);
-        layer_finish<T, N>(e, r, 0, 0, n, sum, res);
+                    for (int j = 0; j < N; ++j) sum[j] += part[w][j];
+            __syncthreads();
+        }
+        if (stores) {
+            float res[N];
+            layer_residual<T, N>(e, r, 0, 0, n, true, res);
+            layer_finish<T, N>(e, r, 0, 0, n, sum, res);
+        }
+        if (!shares || !walk.next(&long_row, &piece)) return;
     }
 }
 
@@ -123,15 +162,17 @@ hipError_t launch_layer_few(const RowsArgs& a, const EpilogueArgs& e, hipStream_
 {
     // (two workgroups to a compute unit, or one; and where the elements of B that are taken are worth the way to LDS)
     const int64_t lds = a.k * a.N * (int64_t)sizeof(T);
-    if (lds > kFewLdsBytes || a.nnz * a.N < 2000000) {
-        layer_few<T, LANES, N, GROUPS, false><<<dim3((unsigned)((a.m + kRowsThreads / LANES - 1) / (kRowsThreads / LANES))), dim3(kRowsThreads), 0, s>>>(a, e);
+    const bool held = lds <= kFewLdsBytes && a.nnz * a.N >= 2000000;
+    const int32_t long_wgs = a.long_room < 256 ? a.long_room : 256;
+    if (!held) {
+        layer_few<T, LANES, N, GROUPS, false><<<dim3((unsigned)((a.m + kRowsThreads / LANES - 1) / (kRowsThreads / LANES) + long_wgs)), dim3(kRowsThreads), 0, s>>>(a, e, long_wgs);
         return hipGetLastError();
     }
     static LdsLimit limit;
     const auto kernel = &layer_few<T, LANES, N, GROUPS, true>;
     const hipError_t err = limit.raise(reinterpret_cast<const void*>(kernel), (int)kFewLdsBytes);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)((a.m + kFewThreads / LANES - 1) / (kFewThreads / LANES))), dim3(kFewThreads), (size_t)lds, s>>>(a, e);
+    kernel<<<dim3((unsigned)((a.m + kFewThreads / LANES - 1) / (kFewThreads / LANES) + long_wgs)), dim3(kFewThreads), (size_t)lds, s>>>(a, e, long_wgs);
     return hipGetLastError();
 }
 template <typename T, int LANES>

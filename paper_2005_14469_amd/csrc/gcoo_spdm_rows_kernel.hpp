@@ -361,6 +361,19 @@ __device__ __forceinline__ void rows_of_wave(const RowsTile<LPR, WIDE, AHEAD, SU
     }
 }
 
+// Which of a tile's long rows workgroup `wg` begins with where XCDs share the tile, the `tile`-th that they share, `slice` workgroups of all such tiles to an XCD: they take them in turns, by the place of a workgroup
+// among those of its XCD, then by XCD.  (In the order of `wg` the first XCD of a tile would have them all; power-law rows, 9958 x 11050, N = 64, 128, 256: 26.5 41.4 48.8 us so, 18.8 24.9 33.3 in turns.)
+__device__ __forceinline__ int32_t rows_slice_turn(int32_t tile, int32_t xcd, int32_t slice, int32_t row_wgs, int32_t wg)
+{
+    const int32_t t0 = tile * row_wgs, t1 = t0 + row_wgs, from = xcd * slice > t0 ? xcd * slice : t0, before = t0 + wg - from;
+    int32_t turn = 0;
+    for (int32_t x = 0; x < 8; ++x) {
+        const int32_t lo = x * slice > t0 ? x * slice : t0, hi = (x + 1) * slice < t1 ? (x + 1) * slice : t1, n = before + (x < xcd ? 1 : 0);
+        if (hi > lo) turn += hi - lo < n ? hi - lo : n;
+    }
+    return turn;
+}
+
 // Item `block`, (tile, wg): rows [wg * kRowsWaves * rpw, ...), `rpw` of them per wave, columns of the tile.  Where the long rows are is a template, since the
 // places in the one kernel cost the other matrices up to 3 % (12000 x 12000, 0.5 %, N = 64: 12.08 and 12.20 us).
 template <int LPR, bool WIDE, int AHEAD, int SUMS, RowsLong LONG, class IO>
@@ -393,16 +406,7 @@ __device__ __forceinline__ void rows_item(const RowsArgs& a, const IO& io, uint3
     int32_t n_front = PLACES ? 0 : (a.long_count ? a.long_count[2] : 0), n_long = PLACES ? a.long_room : (a.long_count ? a.long_count[0] : 0);
     n_front = n_front < a.long_room ? n_front : a.long_room;
     n_long = n_long < a.long_room - n_front ? n_front + n_long : a.long_room;
-    if (__builtin_expect(!PLACES && slice && n_long > 0, 0)) {
-        // The XCDs that share a tile take its long rows in turns: by the place of a workgroup among those of its XCD, then by XCD.  (In the order of `wg` the first XCD of a tile would
-        // have them all; power-law rows, 9958 x 11050, N = 64, 128, 256: 26.5 41.4 48.8 us so, 18.8 24.9 33.3 in turns.)
-        const int32_t t0 = (tile - eights * 8) * row_wgs, t1 = t0 + row_wgs, from = xcd * slice > t0 ? xcd * slice : t0, before = t0 + wg - from;
-        turn = 0;
-        for (int32_t x = 0; x < 8; ++x) {
-            const int32_t lo = x * slice > t0 ? x * slice : t0, hi = (x + 1) * slice < t1 ? (x + 1) * slice : t1, n = before + (x < xcd ? 1 : 0);
-            if (hi > lo) turn += hi - lo < n ? hi - lo : n;
-        }
-    }
+    if (__builtin_expect(!PLACES && slice && n_long > 0, 0)) turn = rows_slice_turn(tile - eights * 8, xcd, slice, row_wgs, wg);
     // (out of the way of matrices without long rows; 12000 x 12000, 0.5 %, N = 64: level, 12.15 us without the hints, 12.13 so)
     if (PLACES || __builtin_expect(n_long > 0, 0)) rows_long_rows<LPR, WIDE, AHEAD, SUMS, LONG, IO>(T, n_front, n_long, turn, row_wgs, long_first, part);
     rows_of_wave<LPR, WIDE, AHEAD, SUMS, IO>(T, w0, wrows, start, wave_row, a.long_row);

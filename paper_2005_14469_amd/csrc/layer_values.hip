@@ -1,6 +1,8 @@
 // The gradient of the stored weights, dvals[e] = sum over n of dZ(row of e, n) B(column of e, n): its kernels and the choice among them.
 #include "gcoo_layer_values.hpp"
 #include "gcoo_layer_device.hpp"
+#include "gcoo_layer_long.hpp"
+#include "gcoo_spdm_rows_kernel.hpp"
 
 namespace gcoo {
 
@@ -13,6 +15,7 @@ namespace gcoo {
 //
 // Bound: the vector caches, through which every entry takes its stretch of B.  The columns of B are cut into tiles of 256 P bytes that stay in an XCD's L2 (4 MB) for as many
 // rows as A has columns; the sums of a tile go to `work` and values_join adds them in the order of the tiles.
+constexpr int kLongPieces = 8;            // of a long row, a workgroup on each
 template <int I>
 __device__ __forceinline__ uint32_t slot_bcast(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + I, 0xf, 0xf, true); }      // row_newbcast:I
 
@@ -225,13 +228,23 @@ struct ValuesTile {
             if (at < end) out[at] = s;
         }
     }
-    // Rows r0 .. r0 + 3 of which those below `end`; ONE: row r0 by all slots.
-    __device__ __forceinline__ void rows(int64_t r0, bool one) const
+    // A piece of a long row, by all slots of the workgroup.
+    __device__ __forceinline__ void long_row(int32_t r, int32_t piece) const
+    {
+        const int32_t beg = a.A.start[r], end = a.A.start[r + 1];
+        const int64_t n = end - beg;
+        Held<T> z[P];
+        row(r, z);
+        entries((uint32_t)(beg + n * piece / kLongPieces) + 16 * (threadIdx.x >> 4), (uint32_t)(beg + n * (piece + 1) / kLongPieces), kValuesThreads, z);
+    }
+    // The row of this slot among rows r0 .. r0 + 3; `one`: r0 for all slots.
+    __device__ __forceinline__ int64_t own(int64_t r0, bool one) const { return one ? r0 : r0 + (lane >> 4); }
+    // Rows r0 .. r0 + 3, the slot's own of the entries [beg, end), but not long ones; `one`: row r0 by all slots.
+    __device__ __forceinline__ void rows(int64_t r0, bool one, int32_t beg, int32_t end) const
     {
         const int slot = lane >> 4;
-        const int64_t m = a.A.m, r = one ? r0 : r0 + slot;
-        int32_t beg = 0, end = 0;
-        if (r < m) { beg = a.A.start[r]; end = a.A.start[r + 1]; }
+        const int64_t m = a.A.m, r = own(r0, one);
+        if (end - beg > a.A.longs.long_row) end = beg;
         Held<T> z[P];
         if (!one) {
             // a row of more entries than the others of the wave together would have them wait: all slots take it
@@ -262,46 +275,65 @@ __global__ __launch_bounds__(kValuesThreads) void values_entries(GradValuesArgs 
 {
     // an XCD walks all rows of one tile before the next, eight tiles side by side; the tiles beyond the last whole eight are cut into eight slices of rows
     const int32_t block = (int32_t)blockIdx.x, xcd = block & 7, at = block >> 3, eights = tiles / 8;
-    int32_t tile, wg;
+    int32_t tile, wg, slice = 0;
     if (at < eights * row_wgs) {
         tile = at / row_wgs * 8 + xcd;
         wg = at - at / row_wgs * row_wgs;
     } else {
-        const int32_t rest = (tiles - eights * 8) * row_wgs, slice = (rest + 7) / 8, x = at - eights * row_wgs, i = xcd * slice + x;
+        const int32_t rest = (tiles - eights * 8) * row_wgs, x = at - eights * row_wgs;
+        slice = (rest + 7) / 8;
+        const int32_t i = xcd * slice + x;
         if (x >= slice || i >= rest) return;
         tile = eights * 8 + i / row_wgs;
         wg = i - i / row_wgs * row_wgs;
     }
     const int64_t wave = (int64_t)wg * (kValuesThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = one ? wave : 4 * wave;
-    if (r0 >= a.A.m) return;
-    if ((int64_t)(tile + 1) * (16 * P * Piece<T>::kElements) > a.N) ValuesTile<T, P, true, ANY>(a, tile, part).rows(r0, one);
-    else ValuesTile<T, P, false, ANY>(a, tile, part).rows(r0, one);
+    const int32_t turn = slice ? rows_slice_turn(tile - eights * 8, xcd, slice, row_wgs, wg) : wg;
+    auto work = [&](const auto& t) {
+        LongWalk<kLongPieces> walk(a.A.longs, a.A.start, a.A.m, turn, row_wgs);
+        const int64_t r = t.own(r0, one);
+        int32_t beg = 0, end = 0, row, piece;
+        if (r < a.A.m) { beg = a.A.start[r]; end = a.A.start[r + 1]; }           // (on their way while the long rows are looked for)
+        while (walk.next(&row, &piece)) t.long_row(row, piece);
+        if (r0 < a.A.m) t.rows(r0, one, beg, end);
+    };
+    if ((int64_t)(tile + 1) * (16 * P * Piece<T>::kElements) > a.N) work(ValuesTile<T, P, true, ANY>(a, tile, part));
+    else work(ValuesTile<T, P, false, ANY>(a, tile, part));
 }
 
 // ---- few columns: a lane per entry ----
 //
-// Up to 64 bytes of a row: sixteen lanes on a row of A, each on every sixteenth entry, the row of dZ in registers of all of them.
+// Up to seven: sixteen lanes on a row of A, each on every sixteenth entry, the row of dZ in registers of all of them.
 template <typename T, int MOST>
 __global__ __launch_bounds__(kValuesThreads) void values_few(GradValuesArgs a)
 {
+    const int N = (int)a.N;
+    const uint32_t kmax = (uint32_t)(a.A.k - 1);
+    auto entries = [&](int64_t r, uint32_t beg, uint32_t end, uint32_t step) {
+        const T* src = static_cast<const T*>(a.dZ) + r * a.lddz;
+        float z[MOST];
+#pragma unroll
+        for (int j = 0; j < MOST; ++j) z[j] = j < N ? widen(src[j]) : 0.0f;
+        for (uint32_t e = beg; e < end; e += step) {
+            const uint32_t c = (uint32_t)a.A.cols[e];
+            const T* b = static_cast<const T*>(a.B) + (int64_t)(c < kmax ? c : kmax) * a.ldb;
+            float s = 0.0f;
+#pragma unroll
+            for (int j = 0; j < MOST; ++j)
+                if (j < N) s = __builtin_fmaf(z[j], widen(b[j]), s);
+            a.dvals[e] = s;
+        }
+    };
+    int32_t row, piece;
+    for (LongWalk<kLongPieces> walk(a.A.longs, a.A.start, a.A.m, (int32_t)blockIdx.x, (int32_t)gridDim.x); walk.next(&row, &piece);) {
+        const int32_t beg = a.A.start[row], end = a.A.start[row + 1];
+        const int64_t n = end - beg;
+        entries(row, (uint32_t)(beg + n * piece / kLongPieces) + threadIdx.x, (uint32_t)(beg + n * (piece + 1) / kLongPieces), kValuesThreads);
+    }
     const int64_t r = (int64_t)blockIdx.x * (kValuesThreads / 16) + (threadIdx.x >> 4);
     if (r >= a.A.m) return;
-    const int N = (int)a.N;
-    const T* src = static_cast<const T*>(a.dZ) + r * a.lddz;
-    float z[MOST];
-#pragma unroll
-    for (int j = 0; j < MOST; ++j) z[j] = j < N ? widen(src[j]) : 0.0f;
-    const uint32_t kmax = (uint32_t)(a.A.k - 1);
-    const uint32_t end = (uint32_t)a.A.start[r + 1];
-    for (uint32_t e = (uint32_t)a.A.start[r] + (threadIdx.x & 15); e < end; e += 16) {
-        const uint32_t c = (uint32_t)a.A.cols[e];
-        const T* b = static_cast<const T*>(a.B) + (int64_t)(c < kmax ? c : kmax) * a.ldb;
-        float s = 0.0f;
-#pragma unroll
-        for (int j = 0; j < MOST; ++j)
-            if (j < N) s = __builtin_fmaf(z[j], widen(b[j]), s);
-        a.dvals[e] = s;
-    }
+    const int32_t beg = a.A.start[r], end = a.A.start[r + 1];
+    if (end - beg <= a.A.longs.long_row) entries(r, (uint32_t)beg + (threadIdx.x & 15), (uint32_t)end, 16);
 }
 
 // ---- by matrix instructions: whole tiles of dZ x B^T, of which the entries are taken ----
@@ -534,11 +566,9 @@ static hipError_t launch_few(const GradValuesArgs& a, hipStream_t s)
 {
     constexpr int64_t rows = kValuesThreads / 16;
     const dim3 grid((unsigned)((a.A.m + rows - 1) / rows)), threads(kValuesThreads);
-    constexpr int most = 64 / sizeof(T);
     if (a.N <= 1) values_few<T, 1><<<grid, threads, 0, s>>>(a);
     else if (a.N <= 4) values_few<T, 4><<<grid, threads, 0, s>>>(a);
-    else if (a.N <= most / 2) values_few<T, most / 2><<<grid, threads, 0, s>>>(a);
-    else values_few<T, most><<<grid, threads, 0, s>>>(a);
+    else values_few<T, 8><<<grid, threads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -574,7 +604,9 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
 {
     const int64_t size = (int64_t)type_bytes(type), bytes = N * size;
     ValuesPlan p{kValuesFew, 1, 1, false, false, 0, 0};
-    if (bytes <= 64) return p;
+    // (from eight columns on a slot of 16 lanes takes 16 bytes a lane and nothing beside them; us, a lane per entry and so: bf16, 8000 x 8000, 5 %, N = 8: 40 38, 16: 71 39, 32: 213 38; 0.5 %, N = 32: 43 10; fp32, 5 %,
+    // N = 4: 27 35, 8: 42 35, 16: 110 35; power-law rows, 16384 x 16384, of 53, bf16, N = 8: 41 36, 32: 136 35)
+    if (N < 8) return p;
     // (buffer loads at multiples of 4 bytes only)
     p.any = (uint64_t)k * (uint64_t)ldb * (uint64_t)size > kRowsMaxBytes || reinterpret_cast<uintptr_t>(B) % 4 != 0 || ldb * size % 4 != 0 || bytes % 4 != 0;
     // (rows of 2-byte elements at odd places: as they are, or copied first)

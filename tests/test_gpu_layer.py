@@ -597,3 +597,61 @@ def test_refuses(module, monkeypatch):
         with pytest.raises((AssertionError, binding.GcooError, ValueError)):
             call()
             print("accepted", i, flush=True)
+
+
+# Long rows (of more than 512 entries and eight times the mean), which whole workgroups share: one of them the first row, one the last.
+LONG = [(1000, 2000, 0.004), (9000, 2500, 0.002), (17000, 6000, 0.0005)]
+
+
+def long_rows(m, k, density):
+    rng = np.random.default_rng(m)
+    mask = rng.random((m, k), dtype=np.float32) < density
+    mask[[0, 17, 18, 500, m - 1]] = rng.random((5, k), dtype=np.float32) < 0.95
+    cells = np.flatnonzero(mask)
+    return workloads.csr_from_cells(m, k, cells, rng.standard_normal(len(cells)).astype(np.float32))
+
+
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,k,density", LONG)
+def test_long_rows(m, k, density, dtype, dense):
+    print(f"long rows: {m} x {k} {density} {dtype} dense={dense}", flush=True)
+    T = TYPES[dtype]
+    arrays = long_rows(m, k, density)
+    row_ptr, cols, vals = arrays
+    lens = np.diff(row_ptr)
+    assert lens[m - 1] > max(512, 8 * (len(vals) // m))
+    W, M = ref.dense(m, k, *arrays)
+    A = binding.gcoo_from_dense(torch.from_numpy(W.astype(np.float32)).to(DEV), 32) if dense else matrix(m, k, arrays)
+    rng = np.random.default_rng(k)
+    for N in (1, 2, 4, 7, 8, 20, 70, 300):
+        B, dZ, R, bias = normal(rng, k, N, dtype=T), normal(rng, m, N, dtype=T), normal(rng, m, N, dtype=T), normal(rng, m)
+        C, Z = Padded(m, N, T, 3, 1), Padded(m, N, T, 1, 0)
+        binding.gcoo_spdm_epilogue(A, B, bias=bias, activation="silu", residual=R, C_out=C.t, Z_out=Z.t)
+        got = binding.gcoo_spdm_grad_values(A, dZ, B)
+        torch.cuda.synchronize()
+        (want, z), (off, off_z) = ref.forward(W, M, lens, ref.f64(B), ref.f64(bias), "silu", ref.f64(R), T)
+        ref.check(C.t, want, off, f"C {N}")
+        ref.check(Z.t, z, off_z, f"Z {N}")
+        ref.check(got, *ref.grad_values(row_ptr, cols, ref.f64(dZ), ref.f64(B)), f"dvals {N}")
+        assert C.whole() and Z.whole()
+        assert torch.equal(binding.gcoo_spdm_grad_values(A, dZ, B), got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_one_long_row_held(dtype):
+    """Long rows with few tokens whose B is kept in LDS."""
+    m, k = 6000, 4000
+    rng = np.random.default_rng(5)
+    mask = rng.random((m, k), dtype=np.float32) < 0.1
+    mask[[3, 4000]] = True
+    mask[[5, 6, m - 1]] = False
+    cells = np.flatnonzero(mask)
+    arrays = workloads.csr_from_cells(m, k, cells, rng.standard_normal(len(cells)).astype(np.float32))
+    assert k > 8 * (len(cells) // m) and len(cells) > 2000000
+    A, (W, M), T = matrix(m, k, arrays), ref.dense(m, k, *arrays), TYPES[dtype]
+    for N in (1, 3):
+        B = normal(rng, k, N, dtype=T)
+        C = binding.gcoo_spdm_epilogue(A, B, activation="gelu")
+        (want, _), (off, _) = ref.forward(W, M, np.diff(arrays[0]), ref.f64(B), None, "gelu", None, T)
+        ref.check(C, want, off, f"C {N}")
