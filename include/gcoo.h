@@ -323,7 +323,8 @@ typedef struct gcoo_epilogue {
  * the residual itself.  The activation takes the sum in fp32, not what Z holds of it.  A row of A without entries gives Z = bias.  A row of B
  * that no stored entry touches does not reach C.  N = 0 or m = 0 is a no-op success.
  * GCOO_EINVAL for an unknown type or activation, a leading dimension below N or, for B, of 2^30 elements and more, a base address that is no multiple of the
- * element size, a missing pointer; GCOO_ENOMEM where work_bytes is too small.
+ * element size, a missing pointer, and where C, Z and the matrices read that they may not overlap begin at one address; GCOO_EHIP, as in the calls below, for 2^26 rows and more or results of 2^36 bytes and more
+ * where a launch would have too many threads; GCOO_ENOMEM where work_bytes is too small.
  * The gradient of B is this product with the transpose of A: gcoo_spdm_epilogue(At, dZ, ..., dB).
  */
 size_t gcoo_spdm_epilogue_bytes(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int64_t N, const gcoo_epilogue* e, const void* C_dev, int64_t ldc);
@@ -334,9 +335,9 @@ int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int
  * The gradient through the epilogue: dZ = dC act'(Z) (m x N), dbias[i] = the sum of row i of dZ before it is rounded to the type.
  *   Z_dev     m x N, ldz >= N: what gcoo_spdm_epilogue() stored; NULL for GCOO_ACT_NONE, where it is not read
  *   dC_dev    m x N, lddc >= N: the gradient of C, which is the gradient of the residual as well
- *   dZ_dev    m x N, lddz >= N, or NULL where only dbias is wanted; may be dC itself (then lddz == lddc)
+ *   dZ_dev    m x N, lddz >= N, or NULL where only dbias is wanted; may be dC itself (then lddz == lddc) or Z itself (lddz == ldz)
  *   dbias_dev m, or NULL
- * relu has the slope 0 at 0.  m = 0 is a no-op success, N = 0 gives dbias = 0.
+ * relu has the slope 0 at 0; where Z is infinite every slope is 0 or 1, to 2^-60.  m = 0 is a no-op success, N = 0 gives dbias = 0.
  */
 size_t gcoo_epilogue_grad_bytes(int64_t m, int64_t N);
 int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const void* Z_dev, int64_t ldz, const void* dC_dev, int64_t lddc,

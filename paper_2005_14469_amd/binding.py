@@ -554,7 +554,7 @@ def gcoo_epilogue_grad(dC: torch.Tensor, Z: torch.Tensor | None = None, activati
     """(dZ, dbias) of C = act(Z) + residual, Z = A x B + bias, from the gradient of C: dZ [m, N] of dC's type, dbias [m] fp32.
 
     Z: what gcoo_spdm_epilogue() stored in Z_out; not needed without an activation, where dZ is dC (and is returned as dC itself unless dZ_out is given).
-    dZ_out may be dC."""
+    dZ_out may be dC or Z."""
     if stream is None and dC.is_cuda:
         got = (_calls or _module()).epilogue_grad(dC, Z, _activation(activation), dZ_out, _raw_stream(dC.get_device()))
         if got is not None:

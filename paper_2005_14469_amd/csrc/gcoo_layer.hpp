@@ -26,6 +26,9 @@ struct RowsView {
 RowsView rows_view(const gcoo_matrix* A);
 int hip_failed(hipError_t e, const char* what);            // keeps the text for gcoo_last_hip_error()
 
+// A launch of more threads than one takes is refused before it is made.
+inline bool too_wide(int64_t workgroups, int threads) { return workgroups > 0xffffffffLL / threads; }
+
 constexpr size_t type_bytes(int type) { return type == GCOO_F32 ? 4 : 2; }
 
 struct EpilogueArgs {

@@ -35,7 +35,7 @@ int check_product(const gcoo::RowsView& A, const void* B, int64_t ldb, int64_t N
     if (N == 0 || A.m == 0) return GCOO_OK;
     if (!C || (A.nnz > 0 && !B)) return GCOO_EINVAL;
     if (e->residual == C && e->residual && e->ldr != ldc) return GCOO_EINVAL;
-    if (e->Z == C) return GCOO_EINVAL;
+    if (e->Z == C || C == B || (e->Z && (e->Z == B || e->Z == e->residual))) return GCOO_EINVAL;
     return GCOO_OK;
 }
 
@@ -80,7 +80,7 @@ int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const voi
     if (reads_z && (ldz < N || !on_elements(Z_dev, type))) return GCOO_EINVAL;
     if (m == 0) return GCOO_OK;
     if (N > 0 && (!dC_dev || (reads_z && !Z_dev))) return GCOO_EINVAL;
-    if (dZ_dev && dZ_dev == dC_dev && lddz != lddc) return GCOO_EINVAL;
+    if (dZ_dev && ((dZ_dev == dC_dev && lddz != lddc) || (reads_z && dZ_dev == Z_dev && lddz != ldz))) return GCOO_EINVAL;
     const int rc = check_work(work, work_bytes, gcoo_epilogue_grad_bytes(m, N));
     if (rc != GCOO_OK || (!dbias_dev && (!dZ_dev || N == 0))) return rc;
     const gcoo::EpilogueGradArgs a{Z_dev, ldz, dC_dev, lddc, dZ_dev, lddz, dbias_dev, m, N, type, activation};

@@ -80,7 +80,7 @@ __device__ __forceinline__ float slope_times(int act, float z, float d)
         case GCOO_ACT_GELU: {
             float e;
             const float f = erfc_and_exp<T>(z, &e);
-            return d * (0.5f * f + z * kDensity0 * e);
+            return d * (0.5f * f + fminf(fmaxf(z, -80.0f), 80.0f) * kDensity0 * e);          // (infinite z, which a sum may be rounded to: 0 or 1)
         }
         case GCOO_ACT_GELU_TANH: return slope_of_gate(z, fminf(fmaxf(z, -8.0f), 8.0f), 2.0f * kGeluA, 2.0f * kGeluA * kGeluB) * d;
         default: return d;

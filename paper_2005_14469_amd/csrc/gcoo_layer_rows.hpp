@@ -141,7 +141,7 @@ template <typename T, int LPR, bool WIDE, int AHEAD, int SUMS>
 hipError_t launch_layer_rows_ahead(const RowsArgs& a, const EpilogueArgs& e, int64_t N4, hipStream_t s)
 {
     const RowsGrid g = rows_grid(a, LPR, LPR * LayerIO<T, T>::COLS, N4);
-    if (g.grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    if (too_wide(g.grid, kRowsThreads)) return hipErrorInvalidConfiguration;
     const auto kernel = !a.long_count && a.long_room > 0 ? layer_rows<T, LPR, WIDE, AHEAD, SUMS, kLongPlaces> : layer_rows<T, LPR, WIDE, AHEAD, SUMS, kLongCounted>;
     kernel<<<dim3((unsigned)g.grid), dim3(kRowsThreads), 0, s>>>(a, LayerIO<T, T>{e}, (int32_t)g.tiles, (int32_t)g.row_wgs, (int32_t)g.rpw, g.wave_row);
     return hipGetLastError();
@@ -163,16 +163,18 @@ hipError_t launch_layer_few(const RowsArgs& a, const EpilogueArgs& e, hipStream_
     // (two workgroups to a compute unit, or one; and where the elements of B that are taken are worth the way to LDS)
     const int64_t lds = a.k * a.N * (int64_t)sizeof(T);
     const bool held = lds <= kFewLdsBytes && a.nnz * a.N >= 2000000;
-    const int32_t long_wgs = a.long_room < 256 ? a.long_room : 256;
+    const int32_t long_wgs = a.long_room < 256 ? a.long_room : 256, threads = held ? kFewThreads : kRowsThreads;
+    const int64_t grid = (a.m + threads / LANES - 1) / (threads / LANES) + long_wgs;
+    if (too_wide(grid, threads)) return hipErrorInvalidConfiguration;
     if (!held) {
-        layer_few<T, LANES, N, GROUPS, false><<<dim3((unsigned)((a.m + kRowsThreads / LANES - 1) / (kRowsThreads / LANES) + long_wgs)), dim3(kRowsThreads), 0, s>>>(a, e, long_wgs);
+        layer_few<T, LANES, N, GROUPS, false><<<dim3((unsigned)grid), dim3(kRowsThreads), 0, s>>>(a, e, long_wgs);
         return hipGetLastError();
     }
     static LdsLimit limit;
     const auto kernel = &layer_few<T, LANES, N, GROUPS, true>;
     const hipError_t err = limit.raise(reinterpret_cast<const void*>(kernel), (int)kFewLdsBytes);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)((a.m + kFewThreads / LANES - 1) / (kFewThreads / LANES) + long_wgs)), dim3(kFewThreads), (size_t)lds, s>>>(a, e, long_wgs);
+    kernel<<<dim3((unsigned)grid), dim3(kFewThreads), (size_t)lds, s>>>(a, e, long_wgs);
     return hipGetLastError();
 }
 template <typename T, int LANES>

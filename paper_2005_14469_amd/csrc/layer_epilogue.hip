@@ -163,6 +163,7 @@ static hipError_t launch_grad_lanes(const EpilogueGradArgs& a, int32_t parts, fl
 {
     constexpr int64_t rows = kPassThreads / LANES;
     const int64_t grid = (a.m + rows - 1) / rows, cols = ((a.N + parts - 1) / parts + 63) / 64 * 64;
+    if (too_wide(grid, kPassThreads)) return hipErrorInvalidConfiguration;
     layer_epilogue_grad<T, LANES><<<dim3((unsigned)grid, (unsigned)parts), dim3(kPassThreads), 0, s>>>(a, parts > 1 ? part : nullptr, cols > 0 ? cols : 64);
     return hipGetLastError();
 }

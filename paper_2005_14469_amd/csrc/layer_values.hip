@@ -555,7 +555,7 @@ static hipError_t launch_entries(const GradValuesArgs& a, const ValuesPlan& plan
     constexpr int64_t waves = kValuesThreads / 64;
     const int64_t rows = plan.one ? waves : 4 * waves, row_wgs = (a.A.m + rows - 1) / rows, tiles = plan.parts;
     const int64_t rest = tiles % 8 * row_wgs, grid = tiles / 8 * 8 * row_wgs + (rest + 7) / 8 * 8;
-    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    if (too_wide(grid, kValuesThreads)) return hipErrorInvalidConfiguration;
     const auto kernel = plan.any ? values_entries<T, P, true> : values_entries<T, P, false>;
     kernel<<<dim3((unsigned)grid), dim3(kValuesThreads), 0, s>>>(a, tiles > 1 ? part : nullptr, (int32_t)tiles, (int32_t)row_wgs, plan.one ? 1 : 0);
     return hipGetLastError();
@@ -565,6 +565,7 @@ template <typename T>
 static hipError_t launch_few(const GradValuesArgs& a, hipStream_t s)
 {
     constexpr int64_t rows = kValuesThreads / 16;
+    if (too_wide((a.A.m + rows - 1) / rows, kValuesThreads)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)((a.A.m + rows - 1) / rows)), threads(kValuesThreads);
     if (a.N <= 1) values_few<T, 1><<<grid, threads, 0, s>>>(a);
     else if (a.N <= 4) values_few<T, 4><<<grid, threads, 0, s>>>(a);
@@ -582,7 +583,7 @@ static hipError_t launch_tiles(const GradValuesArgs& a, const ValuesPlan& plan, 
     const hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel), lds);
     if (e != hipSuccess) return e;
     const int64_t tiles_m = (a.A.m + TM - 1) / TM, tiles_n = (a.A.k + TN - 1) / TN, total = tiles_m * tiles_n * plan.parts;
-    if (total > 0x7ffffff0LL) return hipErrorInvalidConfiguration;
+    if (too_wide(total + 7, 64 * WM * WN) || too_wide((a.A.m + kValuesThreads / 64 - 1) / (kValuesThreads / 64), kValuesThreads)) return hipErrorInvalidConfiguration;
     const int64_t steps = (a.N * (int64_t)sizeof(T) + 127) / 128;
     values_starts<<<dim3((unsigned)((a.A.m + kValuesThreads / 64 - 1) / (kValuesThreads / 64))), dim3(kValuesThreads), 0, s>>>(a.A, (int32_t)tiles_n, TN, starts);
     kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WM * WN), lds, s>>>(a, starts, plan.parts > 1 ? part : a.dvals, (int32_t)tiles_m, (int32_t)tiles_n, plan.parts,

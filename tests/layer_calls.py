@@ -61,7 +61,8 @@ def refusals():
     H.refused(H.L.gcoo_spdm_epilogue(h, AT, 9, 9, None, 2 * AT, 9, 4 * AT, 1 << 50, None), "no epilogue")
     for kw in (dict(type=3), dict(type=-1), dict(activation=5), dict(activation=-1), dict(ldb=8), dict(ldc=8), dict(ldb=1 << 30), dict(N=-1), dict(N=1 << 31, ldb=1 << 31, ldc=1 << 31), dict(B=None), dict(Cp=None),
                dict(residual=3 * AT, ldr=8), dict(Z=3 * AT, ldz=8), dict(residual=2 * AT, ldr=10), dict(Z=2 * AT, ldz=9), dict(bias=AT + 2), dict(B=AT + 2), dict(B=AT + 1, type=BF16), dict(Cp=AT + 3, type=F16),
-               dict(residual=AT + 1, ldr=9, type=F16), dict(Z=AT + 2, ldz=9)):
+               dict(residual=AT + 1, ldr=9, type=F16), dict(Z=AT + 2, ldz=9),
+               dict(B=2 * AT), dict(Z=AT, ldz=9), dict(residual=3 * AT, ldr=9, Z=3 * AT, ldz=9)):
         H.refused(H.forward(h, **kw), kw)
     need = H.forward_bytes(h, type=BF16)
     if need:
@@ -75,8 +76,13 @@ def refusals():
 
     assert H.grad() == OK and H.launches()
     for kw in (dict(m=-1), dict(N=-1), dict(m=1 << 31), dict(N=1 << 31, ldz=1 << 31, lddc=1 << 31, lddz=1 << 31), dict(type=3), dict(act=5), dict(act=-1), dict(lddc=8), dict(ldz=8), dict(lddz=8), dict(dC=None), dict(Z=None),
-               dict(dC=AT + 2), dict(Z=AT + 1, type=BF16), dict(dZ=AT + 1, type=F16), dict(db=AT + 2), dict(dZ=2 * AT, lddz=10)):
+               dict(dC=AT + 2), dict(Z=AT + 1, type=BF16), dict(dZ=AT + 1, type=F16), dict(db=AT + 2), dict(dZ=2 * AT, lddz=10), dict(dZ=AT, lddz=10)):
         H.refused(H.grad(**kw), kw)
+    assert H.grad(dZ=AT) == OK and H.launches()
+    # (more threads than a launch takes; a wide matrix of as many rows has lanes of its own for every row)
+    assert H.grad(m=1 << 28, N=1) == EHIP and not H.launches()
+    assert H.grad(m=(1 << 28) - 16, N=1) == OK and H.launches()
+    assert H.grad(m=1 << 24, N=5000, ldz=5000, lddc=5000, lddz=5000) == EHIP and not H.launches()
     assert H.grad(act=0, Z=None, ldz=0, dZ=None, lddz=0) == OK and H.launches()
     wide = dict(m=1, N=70001, ldz=70001, lddc=70001, lddz=70001)
     need = H.L.gcoo_epilogue_grad_bytes(1, 70001)

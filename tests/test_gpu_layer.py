@@ -1,4 +1,6 @@
 """A layer with sparse weights - the product with its epilogue, its gradients, clipping - against the same in 64 bits (layer_reference.py)."""
+import math
+
 import numpy as np
 import pytest
 
@@ -242,6 +244,9 @@ def test_epilogue_grad(m, N, extra, shift, dtype):
         inside = dC.t.clone()
         _, db2 = binding.gcoo_epilogue_grad(inside, Z=Z.t, activation=act, dZ_out=inside)
         assert torch.equal(inside, dZ) and torch.equal(db, db2)
+        over = Z.t.clone()
+        _, db3 = binding.gcoo_epilogue_grad(dC.t, Z=over, activation=act, dZ_out=over)
+        assert torch.equal(over, dZ) and torch.equal(db, db3)
     same, db = binding.gcoo_epilogue_grad(dC.t)
     assert same is dC.t
 
@@ -264,6 +269,14 @@ def test_epilogue_grad_far_from_zero():
             # (below -30 the value is z exp(z), whose error is that of the exponential, (1.5 |z| + 2) 2^-24 of it: at z = -50 that is 77 2^-24 = 4.8 2^-20, of 1e-20)
             tail = np.where(ref.f64(z) < -30, (1.5 * np.clip(np.abs(ref.f64(z)), 0.0, 400.0) + 2.0) * 2.0 ** -24, 0.0)
             ref.check(y, want, (tail + 2.0 ** -20 + 2.0 ** -24) * np.abs(want) + 2.0 ** -20 * (np.abs(ref.f64(z)) < 30) * np.abs(ref.f64(z)) + 1e-30, act)
+    for T in TYPES.values():
+        # (a sum that the type has no number for is stored as infinite)
+        z = torch.tensor([[-math.inf, math.inf]], device=DEV, dtype=T)
+        for act in binding.ACTIVATIONS:
+            want = [1.0, 1.0] if act == "none" else [0.0, 1.0]
+            got = binding.gcoo_epilogue_grad(torch.ones_like(z), Z=z, activation=act, dZ_out=torch.empty_like(z))[0].double().cpu()[0]
+            # (the logistic functions are taken where their exponential is finite: silu at 80, off by 79 exp(-80) < 2^-109; gelu_tanh at 8, where 2u = 49.3 and (2u)' z = 122: off by 123 exp(-49.3) < 2^-64)
+            assert (got - torch.tensor(want, dtype=torch.float64)).abs().max() < 2.0 ** -60, (T, act, got)
     nan = torch.full((1, 1), float("nan"), device=DEV)
     for act in ("silu", "gelu", "gelu_tanh"):
         assert torch.isnan(binding.gcoo_epilogue_grad(torch.ones_like(nan), Z=nan, activation=act)[0]).all()
