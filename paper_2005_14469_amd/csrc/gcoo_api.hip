@@ -24,6 +24,7 @@
 #include "gcoo_band_build.hpp"
 #include "gcoo_build_kernels.hpp"
 #include "gcoo_layer.hpp"
+#include "gcoo_layer_held.hpp"
 #include "gcoo_order_kernels.hpp"
 #include "gcoo_sched.hpp"
 #include "gcoo_sched_build.hpp"
@@ -1807,6 +1808,13 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
     if (A->inner) A = A->inner;
     const int64_t m = A->m, k = A->k, nnz = A->nnz, size = (int64_t)type_bytes(type);
     if (nnz == 0 || k < 1) return {kProductNone, 0, 0};
+    const TilePlan& tile = tile_plan(m, k, nnz, N);
+    const int held = held_cols(k, N, type);
+    // Few tokens and many entries: B in LDS, in up to four tiles of 16 bytes of a row, where the kernel on tiles of sixteen columns does not serve the matrix.  (us, from the caches and so, bf16: 8000 x 8000, 10 %,
+    // N = 2: 16.7 14.2, 8: 49 20, 16: 50 29, 24: 53 42, 32: 51 47; 2184 x 5230, rows of 458, N = 8: 22 9; below 200000 entries to a tile level, or the way of B to LDS costs more: 8856 x 7930, rows of 8, N = 16: 8.0 12.4;
+    // with the tile kernel 10063 x 1994, rows of 152, N = 16: 12.3 21.  Power-law rows, 16384 x 16384, of 53, N = 4: 20.7 14.1.)
+    const int64_t held_tiles = held > 0 ? (N + held - 1) / held : INT32_MAX;
+    if (held_tiles <= (size == 2 || held == 4 ? 4 : 2) && nnz >= 200000 * held_tiles && tile.row_wgs <= 0) return {kProductHeld, 0, 0};
     if (N < 16 / size) return {kProductRows, 0, 0};
     const int64_t N4 = size == 4 ? N : (N + 1) / 2, padded = (N + 63) / 64 * 64;
     const bool lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0, odd = odd_rows(B, ldb, type);
@@ -1820,7 +1828,6 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
     }
     // (2-byte elements: row by row about 1.45 of what a matrix of half as many 4-byte ones takes where it stays in the caches, since they have to be widened for every entry; us, row by row and on tiles, bf16: 2000 x 2000,
     // N = 2000, 2 %: 25.1 23.9, 5 %: 46.5 38.7; 1000 x 1000, N = 512, 5 %: 9.5 10.0)
-    const TilePlan& tile = tile_plan(m, k, nnz, N);
     if (tile.row_wgs > 0 && tile.time < 0.85 * (size == 4 ? 1.0 : (odd ? 2.0 : 1.45)) * few_columns_rows_time(m, k, nnz, N4, lines)) {
         p = {kProductTile, 0, 0};
         best = std::min(best, tile.time + 1.0);
@@ -1850,6 +1857,7 @@ hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const v
         ldb = plan.ldw;
     }
     const RowsArgs rows = rows_args(A, wide, ldb, N, nullptr, N);
+    if (plan.kernel == kProductHeld) return launch_layer_held(rows, e, s);
     if (plan.kernel == kProductTile) {
         const TilePlan& tile = tile_plan(A->m, A->k, A->nnz, N);
         return launch_layer_tile(rows, e, tile.row_wgs, tile.whole, s);

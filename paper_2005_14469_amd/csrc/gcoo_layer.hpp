@@ -48,9 +48,9 @@ hipError_t launch_widen(const void* src, int64_t lds, int type, float* dst, int6
 // the epilogue of a matrix without entries
 hipError_t launch_epilogue(int64_t m, int64_t N, const EpilogueArgs& e, hipStream_t s);
 
-// Which kernel a product with its epilogue runs: none has entries, row by row (and few columns), on tiles of B in LDS, or by the sixteen-wave kernel, for which a B of 2-byte elements is
+// Which kernel a product with its epilogue runs: none has entries, row by row (and few columns), on a few columns of B held in LDS, on tiles of B in LDS, or by the sixteen-wave kernel, for which a B of 2-byte elements is
 // widened into `work` bytes of the caller's, rows ldw elements apart (and row by row, where that pays for rows at odd places, copied there).
-enum ProductKernel { kProductNone, kProductRows, kProductTile, kProductBand };
+enum ProductKernel { kProductNone, kProductRows, kProductHeld, kProductTile, kProductBand };
 struct ProductPlan { ProductKernel kernel; int64_t ldw; size_t work; };
 ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64_t N, int type);
 hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const void* B, int64_t ldb, int64_t N, const EpilogueArgs& e, void* work, hipStream_t s);

@@ -52,9 +52,8 @@ __device__ __forceinline__ void layer_put(void* base, int64_t at, int first, int
             if (u >= first && u < last) static_cast<T*>(base)[at + u] = narrow<T>(x[u]);
 }
 template <typename T, int COLS>
-__device__ __forceinline__ void layer_finish(const EpilogueArgs& e, int64_t r, int64_t jc, int first, int last, float (&x)[COLS], const float (&res)[COLS])
+__device__ __forceinline__ void layer_finish(const EpilogueArgs& e, float bias, int64_t r, int64_t jc, int first, int last, float (&x)[COLS], const float (&res)[COLS])
 {
-    const float bias = e.bias ? e.bias[r] : 0.0f;
 #pragma unroll
     for (int u = 0; u < COLS; ++u) x[u] += bias;
     if (e.Z) layer_put<T, COLS>(e.Z, r * e.ldz + jc, first, last, x);
@@ -62,6 +61,12 @@ __device__ __forceinline__ void layer_finish(const EpilogueArgs& e, int64_t r, i
 #pragma unroll
     for (int u = 0; u < COLS; ++u) x[u] += res[u];
     layer_put<T, COLS>(e.C, r * e.ldc + jc, first, last, x);
+}
+
+template <typename T, int COLS>
+__device__ __forceinline__ void layer_finish(const EpilogueArgs& e, int64_t r, int64_t jc, int first, int last, float (&x)[COLS], const float (&res)[COLS])
+{
+    layer_finish<T, COLS>(e, e.bias ? e.bias[r] : 0.0f, r, jc, first, last, x, res);
 }
 
 // In the place of RowsPlain; TB: the elements of B, T: of all other matrices.

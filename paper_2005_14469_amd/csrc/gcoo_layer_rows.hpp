@@ -6,9 +6,6 @@
 
 namespace gcoo {
 
-constexpr int kFewThreads = 1024;
-constexpr int64_t kFewLdsBytes = 128 * 1024;
-
 // (registers for four waves of a SIMD, five with eight rows of B in flight: the epilogue and a lane's eight columns do not leave enough for eight)
 template <typename T, int LPR, bool WIDE, int AHEAD, int SUMS, RowsLong LONG>
 __global__ __launch_bounds__(kRowsThreads, AHEAD == 16 ? (LPR == 4 || (LPR == 16 && SUMS == 2) ? 3 : 4) : 5) void layer_rows(RowsArgs a, LayerIO<T, T> io, int32_t tiles, int32_t row_wgs, int32_t rpw, int32_t wave_row)
@@ -18,43 +15,21 @@ __global__ __launch_bounds__(kRowsThreads, AHEAD == 16 ? (LPR == 4 || (LPR == 16
 }
 
 // Few columns: LANES lanes share a row, each takes four adjacent entries at a time with one load each of columns and values, GROUPS such on their way; their sums are added up in a fixed tree.
-// Bound for a single token: the entries, which are all that is read from memory.  The elements of B lie anywhere: from the vector cache a lane's takes a clock of its compute unit, so for many entries the whole
-// of B is brought to LDS first (HELD), which gives 64 lanes theirs in about five (8000 x 8000, 10 %, one token, bf16: 21 us from the cache, 13.4 so, of which reading the entries once at the rate of a large copy takes 10.4).
-// Long rows have workgroups of their own, `long_wgs` behind the others (us, one token: power-law rows, 16384 x 16384, of 53 entries, fp32: 28 10; ten full rows among 20000 of 20 entries: 113 14; with even rows level, but for two to seven
-// tokens on a held B: 8000 x 8000, 10 %, 3 tokens, bf16: 17.1 17.9).
-template <typename T, int LANES, int N, int GROUPS, bool HELD>
-__global__ __launch_bounds__(HELD ? kFewThreads : kRowsThreads, HELD ? 8 : 1) void layer_few(RowsArgs a, EpilogueArgs e, int32_t long_wgs)
+// The elements of B lie anywhere: a lane's takes a clock of its compute unit from the vector cache, so products of many entries hold B in LDS instead (layer_held.hip).
+// Long rows have workgroups of their own, `long_wgs` behind the others (us, one token: power-law rows, 16384 x 16384, of 53 entries, fp32: 28 10; ten full rows among 20000 of 20 entries: 113 14; even rows level).
+template <typename T, int LANES, int N, int GROUPS>
+__global__ __launch_bounds__(kRowsThreads) void layer_few(RowsArgs a, EpilogueArgs e, int32_t long_wgs)
 {
-    constexpr int THREADS = HELD ? kFewThreads : kRowsThreads, SLOTS = THREADS / LANES;
+    constexpr int SLOTS = kRowsThreads / LANES;
     const uint32_t kmax = (uint32_t)(a.k - 1);
     const T* B = reinterpret_cast<const T*>(a.B);
     const int n = (int)a.N;
-    extern __shared__ __attribute__((aligned(16))) char few_smem[];
-    T* held = reinterpret_cast<T*>(few_smem);                              // B, its rows one behind the other
     const int32_t wgs = (int32_t)gridDim.x - long_wgs;
     const bool shares = (int32_t)blockIdx.x >= wgs;
     const LongRows longs{a.long_rows, shares ? a.long_count : nullptr, a.long_row, shares ? a.long_room : 0};
     LongWalk<1> walk(longs, a.row_ptr, a.m, (int32_t)blockIdx.x - wgs, long_wgs);
     int32_t long_row = 0, piece;
     if (shares && !walk.next(&long_row, &piece)) return;
-    if constexpr (HELD) {
-        if (a.ldb == n) {
-            // (the last bytes of B by elements)
-            const int64_t all = a.k * n, vecs = all / 8;
-            for (int64_t i = threadIdx.x; i < vecs; i += THREADS) {
-                typename Adjacent<T, 8>::vec x = *reinterpret_cast<const typename Adjacent<T, 8>::vec*>(B + i * 8);
-                typedef T vec __attribute__((ext_vector_type(8)));
-                *reinterpret_cast<vec*>(held + i * 8) = x;
-            }
-            for (int64_t i = vecs * 8 + threadIdx.x; i < all; i += THREADS) held[i] = B[i];
-        } else {
-            for (int64_t c = threadIdx.x; c < a.k; c += THREADS)
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (j < n) held[c * n + j] = B[c * a.ldb + j];
-        }
-        __syncthreads();
-    }
     const uint32_t lane = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     typedef uint32_t cols4 __attribute__((ext_vector_type(4), aligned(4)));
     typedef float vals4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -102,7 +77,7 @@ __global__ __launch_bounds__(HELD ? kFewThreads : kRowsThreads, HELD ? 8 : 1) vo
                 for (int q = 0; q < 4; ++q) {
                     const bool in = i + 4 * LANES * g + q < end;
                     const uint32_t col = c[g][q] < kmax ? c[g][q] : kmax;
-                    const T* row = HELD ? held + col * (uint32_t)n : B + (int64_t)col * a.ldb;
+                    const T* row = B + (int64_t)col * a.ldb;
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
                         const float b = in && j < n ? widen(row[j]) : 0.0f;
@@ -160,21 +135,10 @@ hipError_t launch_layer_rows(const RowsArgs& a, const EpilogueArgs& e, int64_t N
 template <typename T, int LANES, int N, int GROUPS>
 hipError_t launch_layer_few(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s)
 {
-    // (two workgroups to a compute unit, or one; and where the elements of B that are taken are worth the way to LDS)
-    const int64_t lds = a.k * a.N * (int64_t)sizeof(T);
-    const bool held = lds <= kFewLdsBytes && a.nnz * a.N >= 2000000;
-    const int32_t long_wgs = a.long_room < 256 ? a.long_room : 256, threads = held ? kFewThreads : kRowsThreads;
-    const int64_t grid = (a.m + threads / LANES - 1) / (threads / LANES) + long_wgs;
-    if (too_wide(grid, threads)) return hipErrorInvalidConfiguration;
-    if (!held) {
-        layer_few<T, LANES, N, GROUPS, false><<<dim3((unsigned)grid), dim3(kRowsThreads), 0, s>>>(a, e, long_wgs);
-        return hipGetLastError();
-    }
-    static LdsLimit limit;
-    const auto kernel = &layer_few<T, LANES, N, GROUPS, true>;
-    const hipError_t err = limit.raise(reinterpret_cast<const void*>(kernel), (int)kFewLdsBytes);
-    if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)grid), dim3(kFewThreads), (size_t)lds, s>>>(a, e, long_wgs);
+    const int32_t long_wgs = a.long_room < 256 ? a.long_room : 256;
+    const int64_t grid = (a.m + kRowsThreads / LANES - 1) / (kRowsThreads / LANES) + long_wgs;
+    if (too_wide(grid, kRowsThreads)) return hipErrorInvalidConfiguration;
+    layer_few<T, LANES, N, GROUPS><<<dim3((unsigned)grid), dim3(kRowsThreads), 0, s>>>(a, e, long_wgs);
     return hipGetLastError();
 }
 template <typename T, int LANES>

@@ -668,3 +668,41 @@ def test_one_long_row_held(dtype):
         C = binding.gcoo_spdm_epilogue(A, B, activation="gelu")
         (want, _), (off, _) = ref.forward(W, M, np.diff(arrays[0]), ref.f64(B), None, "gelu", None, T)
         ref.check(C, want, off, f"C {N}")
+
+
+# B held in LDS: few tokens and many entries
+HELD = [(500, 4000, 1, 0.12, 0, 0), (500, 4000, 1, 0.12, 6, 1), (700, 3000, 2, 0.12, 0, 1), (700, 3000, 2, 0.12, 3, 0), (700, 3000, 3, 0.12, 0, 0), (700, 3000, 4, 0.2, 1, 1), (700, 3000, 5, 0.25, 0, 0), (700, 3000, 7, 0.25, 9, 3),
+        (700, 3000, 8, 0.25, 0, 0), (700, 3000, 8, 0.25, 1, 1), (700, 3001, 11, 0.4, 0, 1), (700, 3001, 16, 0.5, 0, 0), (900, 2999, 27, 0.4, 5, 1), (900, 2999, 32, 0.4, 0, 0), (20000, 400, 3, 0.05, 0, 0),
+        (300, 9980, 8, 0.1, 0, 0), (200, 19900, 4, 0.1, 0, 1), (130, 39000, 2, 0.1, 0, 0), (65, 79000, 1, 0.1, 0, 1)]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("m,k,N,density,extra,shift", HELD)
+def test_forward_held(m, k, N, density, extra, shift, dtype):
+    forward_case(m, k, N, density, "uniform" if N % 2 else "loose", TYPES[dtype], "gelu_tanh", True, N % 3 != 0, N % 2 == 0, extra, shift)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_forward_held_of_rows_that_are_not_finite(dtype):
+    """NaN and infinities in rows of B that no entry touches, the first and the last among them, and behind its columns, reach nothing; C may be the residual."""
+    T, m, k = TYPES[dtype], 400, 3000
+    rng = np.random.default_rng(4)
+    mask = rng.random((m, k), dtype=np.float32) < 0.5
+    mask[:, [0, 77, k - 1]] = False
+    mask[5] = False
+    cells = np.flatnonzero(mask)
+    arrays = workloads.csr_from_cells(m, k, cells, rng.standard_normal(len(cells)).astype(np.float32))
+    A, (W, M) = matrix(m, k, arrays), ref.dense(m, k, *arrays)
+    for N in (1, 3, 4, 7, 8):
+        B = Padded(k, N, T, 2, 1, normal(rng, k, N, dtype=T))
+        B.all[B.all == 7.0] = float("nan")
+        want, off = ref.forward(W, M, np.diff(arrays[0]), ref.f64(B.t), None, "relu", None, T)
+        B.t[0], B.t[77], B.t[k - 1] = float("nan"), float("inf"), -float("inf")
+        C = Padded(m, N, T, 1, 1, normal(rng, m, N, dtype=T))
+        R = C.t.clone()
+        binding.gcoo_spdm_epilogue(A, B.t, activation="relu", residual=C.t, C_out=C.t)
+        torch.cuda.synchronize()
+        w = want[0] + ref.f64(R)
+        ref.check(C.t, w, off[0] + (ref.U[T] + ref.F32) * np.abs(w) + ref.LEAST[T], f"C {N}")
+        assert C.whole()
+        assert torch.equal(C.t[5], R[5])
