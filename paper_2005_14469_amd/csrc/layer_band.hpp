@@ -1,4 +1,5 @@
 // The sixteen-wave product with its epilogue: the kernel of gcoo_spdm_band_kernel.hpp, whose sums go through LDS to the epilogue; instances by type in layer_band_*.hip.
+// Bound: vector instructions, as without the epilogue (8000 x 8000, 10 %, N = 8000, fp32: 2010 us; with bias, gelu, residual and Z, 0.77 GB more: 2165).
 #pragma once
 #include "gcoo_layer_io.hpp"
 #include "gcoo_spdm_band_launch.hpp"

@@ -1,4 +1,5 @@
 // The product with its epilogue by the kernel that works row by row on a tile of B in LDS (gcoo_spdm_tile_kernel.hpp), and its launcher: B comes to LDS in fp32, whatever it is in memory.
+// Bound: bank conflicts, as without the epilogue (1777 x 2301, 3 %, N = 1117, fp16, bias, silu, residual and Z: 22 us; fp32 without them 20 to 22).
 #include "gcoo_layer_io.hpp"
 #include "gcoo_spdm_tile_kernel.hpp"
 
