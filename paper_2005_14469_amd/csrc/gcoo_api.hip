@@ -1819,12 +1819,15 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
     const int64_t N4 = size == 4 ? N : (N + 1) / 2, padded = (N + 63) / 64 * 64;
     const bool lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0, odd = odd_rows(B, ldb, type);
     ProductPlan p{kProductRows, 0, 0};
-    const double even = rows_time(m, k, nnz, N4, lines), copied = 2.0 + 4.0 * (double)k * (double)N / 4.5e6;
+    // Rows of B inside 128-byte lines, wide enough for several tiles and rows of A that are not short: copied to lines first, where the two times differ by more than that takes (us, as they are and so: bf16, 20000 x 20000,
+    // rows of 40, N = 500: 93 70, 1501: 313 172; 12000 x 12000, of 100, N = 700: 121 95; fp32, 20000, of 40, N = 300: 124 73; 12000, of 250, N = 203: 194 130.  Narrower ones lose by it: bf16, 20000, of 15, N = 300: 28 40).
+    const bool ways = N4 >= 200 && nnz > 8 * m;
+    const double even = rows_time(m, k, nnz, N4, lines), copied = (ways ? rows_time(m, k, nnz, N4, true) : even) + 2.0 + 2.0 * (double)size * (double)k * (double)N / 4.5e6;
     double best = odd ? 1.4 * even : even;
-    if (odd && even + copied < best && (uint64_t)k * (uint64_t)padded * 2u <= kRowsMaxBytes) {
+    if (!lines && (odd || ways) && copied < (ways ? 0.9 : 1.0) * best && (uint64_t)k * (uint64_t)padded * (uint64_t)size <= kRowsMaxBytes) {
         p.ldw = padded;
-        p.work = al((size_t)k * (size_t)padded * 2);
-        best = even + copied;
+        p.work = al((size_t)k * (size_t)padded * (size_t)size);
+        best = copied;
     }
     // (2-byte elements: row by row about 1.45 of what a matrix of half as many 4-byte ones takes where it stays in the caches, since they have to be widened for every entry; us, row by row and on tiles, bf16: 2000 x 2000,
     // N = 2000, 2 %: 25.1 23.9, 5 %: 46.5 38.7; 1000 x 1000, N = 512, 5 %: 9.5 10.0)
@@ -1849,9 +1852,10 @@ hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const v
 {
     if (A->inner) A = A->inner;
     if (plan.kernel == kProductNone) return launch_epilogue(A->m, N, e, s);
+    const int64_t size = (int64_t)type_bytes(e.type);
     const float* wide = static_cast<const float*>(B);
     if (plan.work > 0) {
-        const hipError_t err = plan.kernel == kProductBand ? launch_widen(B, ldb, e.type, static_cast<float*>(work), plan.ldw, A->k, N, s) : launch_realign(B, ldb, work, plan.ldw, A->k, N, s);
+        const hipError_t err = plan.kernel == kProductBand ? launch_widen(B, ldb, e.type, static_cast<float*>(work), plan.ldw, A->k, N, s) : launch_realign(B, ldb * size / 2, work, plan.ldw * size / 2, A->k, N * size / 2, s);
         if (err != hipSuccess) return err;
         wide = static_cast<const float*>(work);
         ldb = plan.ldw;

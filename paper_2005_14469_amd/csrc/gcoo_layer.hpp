@@ -42,14 +42,14 @@ struct EpilogueArgs {
     int32_t type, activation;
 };
 
-// dst[r][0 .. N) = src[r][0 .. N) of 2-byte elements, in fp32, or as they are; ldd a multiple of 8
+// dst[r][0 .. N) = src[r][0 .. N) of 2-byte elements (or halves of 4-byte ones), as they are, or in fp32; ldd a multiple of 8
 hipError_t launch_realign(const void* src, int64_t lds, void* dst, int64_t ldd, int64_t rows, int64_t N, hipStream_t s);
 hipError_t launch_widen(const void* src, int64_t lds, int type, float* dst, int64_t ldd, int64_t rows, int64_t N, hipStream_t s);
 // the epilogue of a matrix without entries
 hipError_t launch_epilogue(int64_t m, int64_t N, const EpilogueArgs& e, hipStream_t s);
 
 // Which kernel a product with its epilogue runs: none has entries, row by row (and few columns), on a few columns of B held in LDS, on tiles of B in LDS, or by the sixteen-wave kernel, for which a B of 2-byte elements is
-// widened into `work` bytes of the caller's, rows ldw elements apart (and row by row, where that pays for rows at odd places, copied there).
+// widened into `work` bytes of the caller's, rows ldw elements apart (and row by row, where that pays for rows at odd places or inside 128-byte lines, copied there).
 enum ProductKernel { kProductNone, kProductRows, kProductHeld, kProductTile, kProductBand };
 struct ProductPlan { ProductKernel kernel; int64_t ldw; size_t work; };
 ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64_t N, int type);

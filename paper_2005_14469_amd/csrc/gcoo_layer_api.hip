@@ -100,12 +100,12 @@ int check_values(const gcoo::RowsView& A, const void* dZ, int64_t lddz, const vo
 
 // Where the tiles of a row begin, then the sums of the parts, then a copy of B.
 struct ValuesWork { size_t part, copy, total; };
-ValuesWork values_work(const gcoo::RowsView& A, const gcoo::ValuesPlan& p)
+ValuesWork values_work(const gcoo::RowsView& A, const gcoo::ValuesPlan& p, int type)
 {
     ValuesWork w;
     w.part = aligned((size_t)p.starts * 4);
     w.copy = w.part + (p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0);
-    w.total = w.copy + aligned((size_t)A.k * (size_t)p.ldw * 2);
+    w.total = w.copy + aligned((size_t)A.k * (size_t)p.ldw * gcoo::type_bytes(type));
     return w;
 }
 
@@ -118,7 +118,7 @@ size_t gcoo_spdm_grad_values_bytes(const gcoo_matrix* A, const void* dZ_dev, int
     if (!A) return 0;
     const gcoo::RowsView v = gcoo::rows_view(A);
     if (check_values(v, dZ_dev, lddz, B_dev, ldb, N, type) != GCOO_OK || v.nnz == 0) return 0;
-    return values_work(v, gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb)).total;
+    return values_work(v, gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb), type).total;
 }
 
 int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz, const void* B_dev, int64_t ldb, int64_t N, int type,
@@ -131,7 +131,7 @@ int gcoo_spdm_grad_values(const gcoo_matrix* A, const void* dZ_dev, int64_t lddz
     if (!on_floats(dvals_dev) || (v.nnz > 0 && !dvals_dev)) return GCOO_EINVAL;
     if (v.nnz == 0) return GCOO_OK;
     const gcoo::ValuesPlan plan = gcoo::values_plan(v.m, v.k, v.nnz, N, type, B_dev, ldb);
-    const ValuesWork w = values_work(v, plan);
+    const ValuesWork w = values_work(v, plan, type);
     rc = check_work(work, work_bytes, w.total);
     if (rc != GCOO_OK) return rc;
     const gcoo::GradValuesArgs a{v, dZ_dev, lddz, B_dev, ldb, N, type, dvals_dev};

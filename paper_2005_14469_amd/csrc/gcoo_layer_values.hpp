@@ -30,7 +30,7 @@ struct ValuesPlan {
     int64_t ldw;           // not 0: B is copied first, to rows that many elements apart
 };
 ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb);
-// starts: plan.starts words; part: parts x nnz sums where there is more than one part; copy: k x ldw elements of 2 bytes where ldw is not 0
+// starts: plan.starts words; part: parts x nnz sums where there is more than one part; copy: k x ldw elements where ldw is not 0
 hipError_t launch_grad_values(const GradValuesArgs& a, const ValuesPlan& plan, int32_t* starts, float* part, void* copy, hipStream_t s);
 
 }  // namespace gcoo

@@ -598,7 +598,8 @@ static hipError_t launch_tiles(const GradValuesArgs& a, const ValuesPlan& plan, 
 // m x k x N, then the entries one by one.  Against 126 products (256 to 8000 rows and columns, N = 64 to 8000, 0.5 to 20 % stored, bf16 and fp32) the one so chosen takes 1.5 % longer than the faster of
 // the two on average (bf16, us, entries and tiles: 8000 x 8000, N = 8000, 1 %: 545 977, 5 %: 2226 1011; 4000 x 4000, N = 4000, 2 %: 131 147, 5 %: 296 148; 2000 x 2000, N = 512, 5 %: 16 20, 10 %: 24 21;
 // fp32: 8000 x 8000, N = 8000, 5 %: 4411 8088, 20 %: 16597 8141; 2000 x 2000, N = 4000, 10 %: 246 272).
-static double entries_time(double nnz, double rows, double bytes, bool odd16) { return 5.0 + nnz * bytes / (odd16 ? 12.5e6 : 22e6) + rows * bytes / 5e6; }
+// `slower`: what rows at odd places (1.76) or inside 128-byte lines, of which a tile takes one more than it has bytes for, make of the former.
+static double entries_time(double nnz, double rows, double bytes, double slower) { return 5.0 + nnz * bytes * slower / 22e6 + rows * bytes / 5e6; }
 static double tiles_time(double m, double k, double nnz, double N, int type)
 {
     return (type == GCOO_F32 ? 15.0 : 12.0) + 2.0 * m * k * N / (type == GCOO_F32 ? 0.122e9 : 0.9e9) + nnz * 5e-6;
@@ -613,10 +614,13 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
     if (N < 8) return p;
     // (buffer loads at multiples of 4 bytes only)
     p.any = (uint64_t)k * (uint64_t)ldb * (uint64_t)size > kRowsMaxBytes || reinterpret_cast<uintptr_t>(B) % 4 != 0 || ldb * size % 4 != 0 || bytes % 4 != 0;
-    // (rows of 2-byte elements at odd places: as they are, or copied first)
-    const bool odd = odd_rows(B, ldb, type);
-    const double as_is = entries_time((double)nnz, (double)(m + k), (double)bytes, odd), copied = entries_time((double)nnz, (double)(m + k), (double)bytes, false) + 2.0 + 4.0 * (double)k * (double)N / 4.5e6;
-    const bool copies = odd && copied < as_is;
+    // Rows of 2-byte elements at odd places, and rows inside lines where there are several tiles: as they are, or copied first (us, as they are and so: 20000 x 20000, rows of 40: bf16, N = 700: 145 99, fp32, N = 300: 124 87;
+    // 12000 x 12000, rows of 100, bf16, N = 1000: 168 143; 6000 x 6000, rows of 40, N = 1000: 37 as they are, 38 so).
+    const bool odd = odd_rows(B, ldb, type), lines = ldb * size % 128 == 0 && reinterpret_cast<uintptr_t>(B) % 128 == 0;
+    const double inside = lines || bytes <= 1024 ? 1.0 : 1.0 + (double)k / 40000.0, slower = odd && inside < 1.76 ? 1.76 : inside;
+    const double as_is = entries_time((double)nnz, (double)(m + k), (double)bytes, slower);
+    const double copied = entries_time((double)nnz, (double)(m + k), (double)bytes, 1.0) + 2.0 + 2.0 * (double)size * (double)k * (double)N / 4.5e6;
+    const bool copies = copied < (odd ? 1.0 : 0.95) * as_is;
     if (tiles_time((double)m, (double)k, (double)nnz, (double)N, type) < (copies ? copied : as_is)) {
         // tiles of 256 x 256 where they fill the compute units, else of 128 x 128 and as many parts of N as fill them twice, of four steps and more
         p.kernel = kValuesTiles;
@@ -632,7 +636,7 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
     p.kernel = kValuesEntries;
     if (copies) {
         p.ldw = (N + 63) / 64 * 64;
-        p.any = (uint64_t)k * (uint64_t)p.ldw * 2u > kRowsMaxBytes || bytes % 4 != 0;
+        p.any = (uint64_t)k * (uint64_t)p.ldw * (uint64_t)size > kRowsMaxBytes || bytes % 4 != 0;
     }
     if (bytes <= 1024) p.pieces = bytes <= 256 ? 1 : (bytes <= 512 ? 2 : 4);
     else p.pieces = k <= 3500 ? 4 : (k <= 10000 ? 2 : 1);
@@ -646,7 +650,8 @@ hipError_t launch_grad_values(const GradValuesArgs& args, const ValuesPlan& plan
     GradValuesArgs a = args;
     hipError_t e = hipSuccess;
     if (plan.ldw > 0) {
-        e = launch_realign(a.B, a.ldb, copy, plan.ldw, a.A.k, a.N, s);
+        const int64_t halves = (int64_t)type_bytes(a.type) / 2;
+        e = launch_realign(a.B, a.ldb * halves, copy, plan.ldw * halves, a.A.k, a.N * halves, s);
         if (e != hipSuccess) return e;
         a.B = copy;
         a.ldb = plan.ldw;

@@ -54,7 +54,7 @@ def slope(name, z):
 KERNELS = [((4000, 4000, 4000, 0.05, "uniform", "f32 bf16 f16"), "layer_bandI{}Li4ELb0ELb1E"), ((6000, 6000, 6001, 0.02, "uniform", "f32 bf16 f16"), "layer_bandI{}Li4ELb0ELb0E"), ((6000, 6000, 6000, 0.01, "uniform", "f32"), "layer_bandI{}Li2"),
            ((9000, 9000, 9000, 0.0057, "zipf", "f32"), "layer_rows_allI{}"), ((6000, 6000, 6000, 0.02, "heavy", "f32 bf16 f16"), "layer_rows_allI{}"), ((6000, 6000, 5001, 0.02, "heavy", "f32 bf16 f16"), "layer_rows_allI{}"),
            ((4500, 4500, 2000, 0.003, "uniform", "bf16 f16"), "layer_rowsI{}Li32ELb0ELi8E"), ((4500, 4500, 2000, 0.008, "uniform", "bf16 f16"), "layer_rowsI{}Li32ELb0ELi16E"), ((5500, 5500, 2000, 0.006, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb0ELi16E"),
-           ((4500, 4500, 2001, 0.003, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb1E"), ((8000, 8000, 40, 0.002, "uniform", "bf16 f16"), "layer_rowsI{}Li8E"), ((8000, 8000, 21, 0.002, "uniform", "f32"), "layer_rowsI{}Li8E"),
+           ((4500, 4500, 2001, 0.003, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb1E"), ((6000, 6000, 500, 0.042, "uniform", "f32 bf16 f16"), "layer_realign"), ((6000, 6000, 301, 0.042, "uniform", "f32"), "layer_realign"), ((8000, 8000, 40, 0.002, "uniform", "bf16 f16"), "layer_rowsI{}Li8E"), ((8000, 8000, 21, 0.002, "uniform", "f32"), "layer_rowsI{}Li8E"),
            ((17000, 5000, 22, 0.002, "uniform", "bf16 f16"), "layer_rowsI{}Li4E"), ((5000, 5000, 1000, 0.004, "uniform", "bf16 f16"), "layer_rowsI{}Li16ELb0ELi8E"), ((3000, 9000, 300, 0.02, "zipf", "bf16 f16"), "layer_rowsI{}"),
            ((3000, 9000, 301, 0.02, "heavy", "f32 bf16 f16"), "layer_rowsI{}"),
            ((3000, 4000, 1, 0.2, "uniform", "f32 bf16 f16"), "layer_heldI{}Li64ELi1E"), ((3000, 3001, 2, 0.15, "loose", "f32 bf16 f16"), "layer_heldI{}Li64ELi2E"), ((3000, 3001, 3, 0.15, "loose", "f32 bf16 f16"), "layer_heldI{}Li64ELi4E"),
@@ -65,7 +65,7 @@ KERNELS = [((4000, 4000, 4000, 0.05, "uniform", "f32 bf16 f16"), "layer_bandI{}L
 # the gradient of the stored weights
 VALUES_KERNELS = [((4000, 3900, 300, 0.2, "uniform", "bf16 f16"), "values_tilesI{}Li2ELi4ELi4"), ((3600, 4100, 513, 0.1, "loose", "bf16 f16"), "values_tilesI{}Li2ELi4ELi4"), ((1100, 1030, 1500, 0.4, "loose", "f32 bf16 f16"), "values_tilesI{}Li2ELi2ELi2"),
                   ((1000, 12000, 1500, 0.003, "uniform", "f32 bf16 f16"), "values_entriesI{}Li1E"), ((3000, 5000, 2001, 0.004, "zipf", "f32 bf16 f16"), "values_entriesI{}Li2E"), ((3000, 3000, 1200, 0.004, "zipf", "f32 bf16 f16"), "values_entriesI{}Li4E"),
-                  ((9000, 3000, 24, 0.01, "loose", "f32 bf16 f16"), "values_"), ((3000, 3000, 1200, 0.01, "heavy", "f32 bf16 f16"), "values_entriesI{}Li4E"), ((5000, 4000, 2001, 0.01, "uniform", "bf16 f16"), "layer_realign")]
+                  ((9000, 3000, 24, 0.01, "loose", "f32 bf16 f16"), "values_"), ((3000, 3000, 1200, 0.008, "heavy", "f32 bf16 f16"), "values_entriesI{}Li4E"), ((6000, 6000, 500, 0.042, "uniform", "f32"), "layer_realign"), ((6000, 6000, 501, 0.042, "loose", "f32"), "layer_realign"), ((5000, 4000, 2001, 0.01, "uniform", "bf16 f16"), "layer_realign")]
 MANGLED = {"f32": "f", "bf16": "DF16b", "f16": "DF16_"}
 
 
