@@ -1808,7 +1808,8 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
     if (A->inner) A = A->inner;
     const int64_t m = A->m, k = A->k, nnz = A->nnz, size = (int64_t)type_bytes(type);
     if (nnz == 0 || k < 1) return {kProductNone, 0, 0};
-    const TilePlan& tile = tile_plan(m, k, nnz, N);
+    const bool halves = type == GCOO_F16 && N >= 2 * kTileCols;                      // (in LDS)
+    const TilePlan& tile = tile_plan(m, k, nnz, halves ? (N + 1) / 2 : N);
     const int held = held_cols(k, N, type);
     // Few tokens and many entries: B in LDS, in up to four tiles of 16 bytes of a row, where the kernel on tiles of sixteen columns does not serve the matrix.  (us, from the caches and so, bf16: 8000 x 8000, 10 %,
     // N = 2: 16.7 14.2, 8: 49 20, 16: 50 29, 24: 53 42, 32: 51 47; 2184 x 5230, rows of 458, N = 8: 22 9; below 200000 entries to a tile level, or the way of B to LDS costs more: 8856 x 7930, rows of 8, N = 16: 8.0 12.4;
@@ -1830,8 +1831,9 @@ ProductPlan product_plan(const gcoo_matrix* A, const void* B, int64_t ldb, int64
         best = copied;
     }
     // (2-byte elements: row by row about 1.45 of what a matrix of half as many 4-byte ones takes where it stays in the caches, since they have to be widened for every entry; us, row by row and on tiles, bf16: 2000 x 2000,
-    // N = 2000, 2 %: 25.1 23.9, 5 %: 46.5 38.7; 1000 x 1000, N = 512, 5 %: 9.5 10.0)
-    if (tile.row_wgs > 0 && tile.time < 0.85 * (size == 4 ? 1.0 : (odd ? 2.0 : 1.45)) * few_columns_rows_time(m, k, nnz, N4, lines)) {
+    // N = 2000, 2 %: 25.1 23.9, 5 %: 46.5 38.7; 1000 x 1000, N = 512, 5 %: 9.5 10.0.  fp16 in LDS as it is: over 204 products of 500 to 2500 columns, 1 to 25 %, 8 % less time than with fp32 there, and 1.0 in the place of 1.45
+    // costs 2.7 % against the fastest of all, 1.2 4.1 %)
+    if (tile.row_wgs > 0 && tile.time < 0.85 * (size == 4 ? 1.0 : (odd ? 1.4 : 1.0) * (halves ? 1.0 : 1.45)) * few_columns_rows_time(m, k, nnz, N4, lines)) {
         p = {kProductTile, 0, 0};
         best = std::min(best, tile.time + 1.0);
     }
@@ -1862,6 +1864,10 @@ hipError_t launch_product(const gcoo_matrix* A, const ProductPlan& plan, const v
     }
     const RowsArgs rows = rows_args(A, wide, ldb, N, nullptr, N);
     if (plan.kernel == kProductHeld) return launch_layer_held(rows, e, s);
+    if (plan.kernel == kProductTile && e.type == GCOO_F16 && N >= 2 * kTileCols) {
+        const TilePlan& tile = tile_plan(A->m, A->k, A->nnz, (N + 1) / 2);
+        return launch_layer_tile_halves(rows, e, tile.row_wgs, tile.whole, s);
+    }
     if (plan.kernel == kProductTile) {
         const TilePlan& tile = tile_plan(A->m, A->k, A->nnz, N);
         return launch_layer_tile(rows, e, tile.row_wgs, tile.whole, s);

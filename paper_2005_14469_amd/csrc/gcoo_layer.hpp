@@ -63,6 +63,7 @@ hipError_t launch_layer_rows_f32(const RowsArgs& a, const EpilogueArgs& e, hipSt
 hipError_t launch_layer_rows_bf16(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s);
 hipError_t launch_layer_rows_f16(const RowsArgs& a, const EpilogueArgs& e, hipStream_t s);
 hipError_t launch_layer_tile(const RowsArgs& a, const EpilogueArgs& e, int64_t row_wgs, bool whole, hipStream_t s);
+hipError_t launch_layer_tile_halves(const RowsArgs& a, const EpilogueArgs& e, int64_t row_wgs, bool whole, hipStream_t s);      // of a product of half as many columns
 hipError_t launch_layer_band_f32(const BandArgs& a, const RowsArgs& rows, const EpilogueArgs& e, hipStream_t s);
 hipError_t launch_layer_band_bf16(const BandArgs& a, const RowsArgs& rows, const EpilogueArgs& e, hipStream_t s);
 hipError_t launch_layer_band_f16(const BandArgs& a, const RowsArgs& rows, const EpilogueArgs& e, hipStream_t s);

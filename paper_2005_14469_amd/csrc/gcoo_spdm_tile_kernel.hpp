@@ -70,27 +70,38 @@ struct TileBatch {
     }
 };
 
+// What lies in LDS: four fp32 columns to a lane, as here, or, for an operator of a sparse layer, eight of 2 bytes (layer_tile.hip).
+struct TileFloats {
+    static constexpr int kCols = 4;
+    typedef tile_f32x4 Read;
+    static __device__ __forceinline__ void add(const Read& x, float w, float (&acc)[4])
+    {
+        for (int u = 0; u < 4; ++u) acc[u] = __builtin_fmaf(w, x[u], acc[u]);
+    }
+};
+
 // Entries I .. I + 3 of the batch.  (Eight reads of LDS in front of the multiply-adds need more than 64 registers: 1 to 5 % slower.)
-template <int I>
-__device__ __forceinline__ void tile_step(const TileBatch& b, const char* at, float (&acc)[4])
+template <int I, class IN>
+__device__ __forceinline__ void tile_step(const TileBatch& b, const char* at, float (&acc)[IN::kCols])
 {
-    tile_f32x4 x[4];
-#define TILE_READ(J) x[J] = *reinterpret_cast<const tile_f32x4*>(at + tile_bcast<I + J>(b.c));
+    typename IN::Read x[4];
+#define TILE_READ(J) x[J] = *reinterpret_cast<const typename IN::Read*>(at + tile_bcast<I + J>(b.c));
     TILE_READ(0) TILE_READ(1) TILE_READ(2) TILE_READ(3)
 #undef TILE_READ
 #define TILE_FMA(J)                                                                                          \
     {                                                                                                        \
         uint32_t w = tile_bcast<I + J>(b.v);                                                                 \
         asm("" : "+v"(w));                     /* a move of its own, not four multiply-adds with DPP */      \
-        for (int u = 0; u < 4; ++u) acc[u] = __builtin_fmaf(__uint_as_float(w), x[J][u], acc[u]);            \
+        IN::add(x[J], __uint_as_float(w), acc);                                                              \
     }
     TILE_FMA(0) TILE_FMA(1) TILE_FMA(2) TILE_FMA(3)
 #undef TILE_FMA
 }
 
 // Adds the entries [beg, end) of the slot's row.  `next` holds the first batch already; on return it holds the one at `more`, requested in front of the last entries.
+template <class IN>
 __device__ __forceinline__ void tile_entries(__amdgpu_buffer_rsrc_t cols, __amdgpu_buffer_rsrc_t vals, TileBatch& next, int32_t beg, int32_t end, int32_t more, uint32_t kmax,
-                                             const char* at, int lane, float (&acc)[4])
+                                             const char* at, int lane, float (&acc)[IN::kCols])
 {
     int32_t left = end - beg;
     while (true) {
@@ -99,12 +110,12 @@ __device__ __forceinline__ void tile_entries(__amdgpu_buffer_rsrc_t cols, __amdg
         const bool last = !__any(left > 16);
         next.request(cols, vals, last ? more : beg, lane);
         now.offsets(left, kmax, lane);
-        tile_step<0>(now, at, acc);
+        tile_step<0, IN>(now, at, acc);
         if (__any(left > 4)) {
-            tile_step<4>(now, at, acc);
+            tile_step<4, IN>(now, at, acc);
             if (__any(left > 8)) {
-                tile_step<8>(now, at, acc);
-                if (__any(left > 12)) tile_step<12>(now, at, acc);
+                tile_step<8, IN>(now, at, acc);
+                if (__any(left > 12)) tile_step<12, IN>(now, at, acc);
             }
         }
         if (last) return;
@@ -114,6 +125,7 @@ __device__ __forceinline__ void tile_entries(__amdgpu_buffer_rsrc_t cols, __amdg
 
 // B and C as they are here: pieces of four fp32 columns, and the sums.  The operators of a sparse layer have others (layer_tile.hip).
 struct TilePlain {
+    typedef TileFloats In;
     __amdgpu_buffer_rsrc_t B;
     uint32_t ldb4;
     __device__ __forceinline__ TilePlain(const RowsArgs& a, int32_t jb)
@@ -142,13 +154,15 @@ struct TilePlain {
 template <class MakeIO>
 __device__ __forceinline__ void tile_item(const RowsArgs& a, int32_t row_wgs, int32_t rows, int32_t total, int32_t long_steps, MakeIO&& make_io)
 {
+    typedef typename decltype(make_io(0))::In In;
+    constexpr int32_t kCols = In::kCols, kTile = kTileLanes * kCols;
     extern __shared__ __attribute__((aligned(16))) char tile_smem[];
     __shared__ int32_t counts[2];                                  // long rows, items taken
     const int32_t per = (int32_t)(gridDim.x >> 3), block = (int32_t)(blockIdx.x & 7u) * per + (int32_t)(blockIdx.x >> 3);
     if (block >= total) return;                                    // the whole workgroup
     const int32_t tile = block / row_wgs, wg = block - tile * row_wgs, n = (int32_t)a.N;
     // the last tile of a B that is no multiple of a tile wide begins where it can hold a whole one
-    const int32_t j0 = tile * kTileCols, jb = j0 > n - kTileCols ? n - kTileCols : j0;
+    const int32_t j0 = tile * kTile, jb = j0 > n - kTile ? n - kTile : j0;
     const int32_t t = (int32_t)threadIdx.x, lane = t & 63, k = (int32_t)a.k, pieces = k * kTileLanes;
     const int64_t r0 = (int64_t)wg * rows;
     const int32_t mine = (int32_t)(a.m - r0 < rows ? a.m - r0 : rows);
@@ -202,7 +216,7 @@ __device__ __forceinline__ void tile_item(const RowsArgs& a, int32_t row_wgs, in
     const uint32_t kmax = (uint32_t)(k - 1);
     __amdgpu_buffer_rsrc_t cols = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(a.cols), 0, (int)(uint32_t)(a.nnz * 4), 0x00027000);
     __amdgpu_buffer_rsrc_t vals = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.vals), 0, (int)(uint32_t)(a.nnz * 4), 0x00027000);
-    const int32_t jc = jb + sl * 4;                                // the lane's first column; it stores those from j0 on
+    const int32_t jc = jb + sl * kCols;                            // the lane's first column; it stores those from j0 on
     const int32_t n_long = counts[0], items = n_long + (mine - n_long + kTileSlots - 1) / kTileSlots;
     // What the slot does of item x of the workgroup: a long row, shared by the slots, or sixteen rows.  row < 0: nothing.
     struct Item { int32_t row, beg, end; };
@@ -238,13 +252,13 @@ __device__ __forceinline__ void tile_item(const RowsArgs& a, int32_t row_wgs, in
         if (lane == 0) x2 = kTileWaves + atomicAdd(&counts[1], 1);
         x2 = __builtin_amdgcn_readfirstlane(x2);
         const Item then = item_of(x2);
-        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        tile_entries(cols, vals, next, now.beg, now.end, then.beg, kmax, at, lane, acc);
+        float acc[kCols] = {};
+        tile_entries<In>(cols, vals, next, now.beg, now.end, then.beg, kmax, at, lane, acc);
         if (x < n_long) {
 #pragma unroll
             for (int d = kTileLanes; d < 64; d <<= 1)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) acc[u] += __shfl_xor(acc[u], d, 64);
+                for (int u = 0; u < kCols; ++u) acc[u] += __shfl_xor(acc[u], d, 64);
         }
         if (now.row >= 0 && (x >= n_long || slot == 0)) {
             io.store(a, r0 + now.row, jc, j0, acc);

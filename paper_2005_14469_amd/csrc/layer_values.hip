@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kValuesThreads) void values_few(GradValuesArgs a)
 // there to the matrix instructions by 16 bytes per lane.  Where those bytes lie in a step is the same for both operands, so the instructions may take them in any order.
 // 16 bytes of row r are at piece ^ (r / 2 mod 8) of its 128 in LDS: sixteen lanes that read one piece of sixteen rows, and sixteen that write two rows, meet all 64 banks once.
 // For few tiles N is cut into parts, whose sums are joined afterwards.
-// Bound: the matrix instructions (4001 x 3999, 5 %, N = 4003, bf16: 141 to 146 us with starts and join, 0.8 of the rate of a large product; 8000 x 8000, 10 %, N = 8000: bf16 1.0 ms, fp32 8.1 ms, 127 of 153 TFLOP/s).
+// Bound: the matrix instructions (4001 x 3999, 5 %, N = 4003, bf16: 141 to 148 us with starts and join, 0.8 of the rate of a large product; 8000 x 8000, 10 %, N = 8000: bf16 1.0 ms, fp32 8.1 ms, 127 of 153 TFLOP/s).
 template <typename T> struct Mfma;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <> struct Mfma<bf16_t> {

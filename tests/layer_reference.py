@@ -61,7 +61,8 @@ KERNELS = [((4000, 4000, 4000, 0.05, "uniform", "f32 bf16 f16"), "layer_bandI{}L
            ((3000, 3001, 31, 0.15, "loose", "bf16 f16"), "layer_heldI{}Li64ELi8E"), ((3000, 3001, 15, 0.15, "loose", "f32"), "layer_heldI{}Li64ELi4E"), ((600, 9900, 7, 0.1, "uniform", "bf16 f16"), "layer_heldI{}Li64ELi8E"),
            ((30000, 800, 2, 0.1, "loose", "f32 bf16 f16"), "layer_heldI{}Li16ELi2E"), ((40000, 700, 8, 0.02, "uniform", "bf16 f16"), "layer_heldI{}Li16ELi8E"), ((40000, 700, 7, 0.02, "uniform", "f32 bf16 f16"), "layer_heldI{}Li16E"),
            ((300, 30000, 6, 0.08, "uniform", "bf16 f16"), "layer_heldI{}Li64ELi2E"), ((300, 30000, 1, 0.05, "uniform", "f32"), "layer_heldI{}Li64ELi1E"), ((3000, 50000, 1, 0.005, "loose", "f32"), "layer_fewI{}Li64ELi1E"),
-           ((3000, 50000, 3, 0.005, "loose", "f32 bf16 f16"), "layer_fewI{}Li64ELi4E"), ((3000, 90000, 7, 0.0001, "uniform", "bf16 f16"), "layer_fewI{}Li16ELi8E"), ((2000, 1900, 1001, 0.05, "uniform", "f32 bf16 f16"), "layer_tileI{}")]
+           ((3000, 50000, 3, 0.005, "loose", "f32 bf16 f16"), "layer_fewI{}Li64ELi4E"), ((3000, 90000, 7, 0.0001, "uniform", "bf16 f16"), "layer_fewI{}Li16ELi8E"), ((2000, 1900, 1001, 0.05, "uniform", "f32 bf16"), "layer_tileI{}"), ((2000, 1900, 1001, 0.05, "uniform", "f16"), "layer_tile_halves"), ((2000, 1000, 33, 0.25, "loose", "f16"), "layer_tile_halves"),
+           ((1000, 2000, 100, 0.1, "heavy", "f16"), "layer_tile_halves"), ((2000, 1900, 20, 0.2, "uniform", "f32 bf16 f16"), "layer_tileI{}")]
 # the gradient of the stored weights
 VALUES_KERNELS = [((4000, 3900, 300, 0.2, "uniform", "bf16 f16"), "values_tilesI{}Li2ELi4ELi4"), ((3600, 4100, 513, 0.1, "loose", "bf16 f16"), "values_tilesI{}Li2ELi4ELi4"), ((1100, 1030, 1500, 0.4, "loose", "f32 bf16 f16"), "values_tilesI{}Li2ELi2ELi2"),
                   ((1000, 12000, 1500, 0.003, "uniform", "f32 bf16 f16"), "values_entriesI{}Li1E"), ((3000, 5000, 2001, 0.004, "zipf", "f32 bf16 f16"), "values_entriesI{}Li2E"), ((3000, 3000, 1200, 0.004, "zipf", "f32 bf16 f16"), "values_entriesI{}Li4E"),
