@@ -290,7 +290,7 @@ int gcoo_export_share(const gcoo_matrix* A, uint32_t* hdr, uint32_t* blocks, int
  * A holds the weights of such a layer (fp32, as everywhere here), B has a column per token.  The dense matrices that a layer passes on are fp32,
  * bfloat16 or float16, one type for all matrices of a call; bias, the gradients of the bias and of the weights, and every sum are fp32, and
  * a result is rounded once, to nearest even, when it is stored.  Matrices are row-major on the device, aligned to their element type, with
- * leading dimensions in elements; any alignment beyond that is served (rows and leading dimensions at multiples of 16 bytes are the fastest).
+ * leading dimensions in elements; any alignment beyond that is served (rows at multiples of 128 bytes are the fastest).
  *
  * These calls launch kernels on `stream` and return, like gcoo_spdm(): they wait for nothing, allocate nothing, copy nothing back and may be recorded into a
  * stream capture.  Results are the same bits from run to run.  `work` is device memory of the caller (256-byte aligned, at least as many bytes as the
