@@ -2,7 +2,7 @@
 
 How far they may be off, u = 2^-24.  With x the exponent that an activation takes (silu z, gelu z^2 / 2, gelu_tanh 2 sqrt(2 / pi) (z + 0.044715 z^3)), the exponential and at most sixteen roundings around it are off by
 16 u of the value.  An exponent formed in fp32 is off by as many u of itself as it has roundings, which the exponential turns into as many |x| u of its value: gelu_tanh has five (two of constants), gelu none in fp32, where
-what the square loses is not left out, and one for the types of 2 bytes.  Those have an exponential of a product and a power of two, 1.5 |x| u more, and a polynomial for gelu that is off by 2^-17.  An exponential
+what the square loses is not left out, and one for the types of 2 bytes.  Those have an exponential of a product and a power of two, 1.5 |x| u more, and a polynomial for gelu that is off by 2^-22.  An exponential
 below 2^-126, which is no normal number, may be 0: times z, that is up to 110, less than 2^-119.  A slope is a sum of two terms of either sign: the bound is of their magnitudes.  The rounding to the type comes on top."""
 import math
 
@@ -50,7 +50,7 @@ def relative(act, z, T):
     x = np.abs(exponent(act, z))
     if T is torch.float32:
         return ({"silu": 0.0, "gelu": 0.0, "gelu_tanh": 5.0}[act] * x + 16.0) * u
-    return ({"silu": 1.5, "gelu": 2.5, "gelu_tanh": 6.5}[act] * x + 16.0) * u + (2.0 ** -17 if act == "gelu" else 0.0)
+    return ({"silu": 1.5, "gelu": 2.5, "gelu_tanh": 6.5}[act] * x + 16.0) * u + (2.0 ** -22 if act == "gelu" else 0.0)
 
 
 def check(act, T, points):
@@ -72,3 +72,8 @@ def test_gelu_in_32_bits():
     """Phi(z) as 1 + erf would have lost every bit at z = -5.5, where gelu is -1e-7."""
     check("gelu", torch.float32, GRID)
     check("gelu", torch.float32, np.linspace(-13.0, -1.0, 50001))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_gelu_in_16_bits(dtype):
+    check("gelu", TYPES[dtype], GRID)
