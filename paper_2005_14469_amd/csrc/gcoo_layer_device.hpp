@@ -22,7 +22,28 @@ auto with_type(int type, F&& f)
     return f(float{});
 }
 
-__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
+// exp(x + more) for x <= 0, `more` a remainder that x is too coarse to hold: the instruction's power of two, off by a unit in the last place, times what the exponent loses by rounding; 0 below 2^-126, where
+// the instruction has no numbers.  (The library's expf, which has them, takes more than twice as many instructions.)
+__device__ __forceinline__ float exp_below(float x, float more = 0.0f)
+{
+    constexpr float hi = 1.44269502f, lo = 1.92596299e-8f, ln2 = 0.693147182f;              // hi + lo = 1 / ln 2
+    const float c = fmaxf(x, -200.0f), h = c * hi, e = __builtin_amdgcn_exp2f(h);
+    return __builtin_fmaf(e, __builtin_fmaf(ln2, __builtin_fmaf(c, lo, __builtin_fmaf(c, hi, -h)), more), e);
+}
+// 1 / x for x >= 1, off by less than a unit in the last place: the instruction's and one step of Newton's.
+__device__ __forceinline__ float reciprocal(float x)
+{
+    const float r = __builtin_amdgcn_rcpf(x);
+    return __builtin_fmaf(__builtin_fmaf(-x, r, 1.0f), r, r);
+}
+// 1 / (1 + exp(-x)).  In fp32 off by 8 2^-24, for negative x as exp(x) / (1 + exp(x)); for types of 2 bytes by single instructions, (1.5 |x| + 2) 2^-24.
+template <typename T>
+__device__ __forceinline__ float logistic(float x)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+    const float e = exp_below(-fabsf(x)), s = reciprocal(1.0f + e);
+    return x < 0.0f ? e * s : s;
+}
 constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f, kDensity0 = 0.3989422804014327f;
 
 // Phi(-a) / exp(-a^2 / 2) and exp(-a^2 / 2), a = |z|, held where the exponential is 0 already (which it is where it is no normal number: what follows would go on with the few bits that are left of it): from these two
@@ -42,12 +63,11 @@ __device__ __forceinline__ GaussTail gauss_tail(float z)
         p = __builtin_fmaf(p, t, 0.107669815f); p = __builtin_fmaf(p, t, 0.12407776f); p = __builtin_fmaf(p, t, 0.123655692f);
         return {p * t, __builtin_amdgcn_exp2f(a * a * -0.72134752f), a};            // -log2(e) / 2
     }
-    const float s = a * a, lost = __builtin_fmaf(a, a, -s), t = 1.0f / __builtin_fmaf(0.27f, a, 1.0f);
+    const float s = a * a, lost = __builtin_fmaf(a, a, -s), t = reciprocal(__builtin_fmaf(0.27f, a, 1.0f));
     float p = 0.0290386342f;
     p = __builtin_fmaf(p, t, -0.126874849f); p = __builtin_fmaf(p, t, 0.170617849f); p = __builtin_fmaf(p, t, -0.0701981857f); p = __builtin_fmaf(p, t, 0.108535729f);
     p = __builtin_fmaf(p, t, 0.0717337355f); p = __builtin_fmaf(p, t, 0.101895243f); p = __builtin_fmaf(p, t, 0.107530423f); p = __builtin_fmaf(p, t, 0.107721426f);
-    const float e = s > 174.6f ? 0.0f : expf(-0.5f * s);
-    return {p * t, __builtin_fmaf(e, -0.5f * lost, e), a};
+    return {p * t, exp_below(-0.5f * s, -0.5f * lost), a};
 }
 
 template <typename T>
@@ -55,12 +75,12 @@ __device__ __forceinline__ float activate(int act, float z)
 {
     switch (act) {
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-        case GCOO_ACT_SILU: return z * logistic(z);
+        case GCOO_ACT_SILU: return z * logistic<T>(z);
         case GCOO_ACT_GELU: {
             const GaussTail g = gauss_tail<T>(z);
             return __builtin_fmaf(-g.a, g.q * g.e, z <= 0.0f ? 0.0f : z);             // max(z, 0) - |z| Phi(-|z|)
         }
-        case GCOO_ACT_GELU_TANH: return z * logistic(2.0f * kGeluA * (z + kGeluB * z * z * z));
+        case GCOO_ACT_GELU_TANH: return z * logistic<T>(2.0f * kGeluA * (z + kGeluB * z * z * z));
         default: return z;
     }
 }

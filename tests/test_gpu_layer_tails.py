@@ -53,7 +53,7 @@ def relative(act, z, T):
     return ({"silu": 1.5, "gelu": 2.5, "gelu_tanh": 6.5}[act] * x + 16.0) * u + (2.0 ** -22 if act == "gelu" else 0.0)
 
 
-def check(act, T, points):
+def check(act, T, points, slopes=True):
     print(f"tails: {act} {T} {points[0]} .. {points[-1]}", flush=True)
     z = torch.from_numpy(points.astype(np.float32)).to(DEV).to(T)[None, :].contiguous()
     one = binding.gcoo_from_csr(1, 1, *[torch.from_numpy(a).to(DEV) for a in (np.array([0, 1], np.int32), np.zeros(1, np.int32), np.ones(1, np.float32))], 32, known_nnz=True)
@@ -61,6 +61,8 @@ def check(act, T, points):
     rel = relative(act, z64, T)
     want = value(act, z64)
     ref.check(binding.gcoo_spdm_epilogue(one, z, activation=act), want, (rel + U * (1.0 + rel)) * np.abs(want) + least, "value")
+    if not slopes:
+        return
     want, both = slope(act, z64)
     ref.check(binding.gcoo_epilogue_grad(torch.ones_like(z), Z=z, activation=act)[0], want, rel * both + U * (np.abs(want) + rel * both) + least, "slope")
 
@@ -77,3 +79,8 @@ def test_gelu_in_32_bits():
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_gelu_in_16_bits(dtype):
     check("gelu", TYPES[dtype], GRID)
+
+
+def test_silu_and_gelu_tanh_in_32_bits():
+    check("silu", torch.float32, np.linspace(-80.0, 80.0, 40001), slopes=False)
+    check("gelu_tanh", torch.float32, GRID, slopes=False)
