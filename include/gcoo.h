@@ -289,7 +289,9 @@ int gcoo_export_share(const gcoo_matrix* A, uint32_t* hdr, uint32_t* blocks, int
  *
  * A holds the weights of such a layer (fp32, as everywhere here), B has a column per token.  The dense matrices that a layer passes on are fp32,
  * bfloat16 or float16, one type for all matrices of a call; bias, the gradients of the bias and of the weights, and every sum are fp32, and
- * a result is rounded once, to nearest even, when it is stored.  Matrices are row-major on the device, aligned to their element type, with
+ * a result is rounded once, to nearest even, when it is stored.  An activation of the sum is computed in fp32: off by 16 2^-24 of its value, gelu_tanh by
+ * 5 |2u| 2^-24 more; for the types of 2 bytes by 2.5 |x| 2^-24 more, x the exponent that it takes (z, z^2 / 2, 2u); an exponential below 2^-126 may be 0.  A slope
+ * is off by as much of the magnitudes of the two terms that it is the sum of.  Matrices are row-major on the device, aligned to their element type, with
  * leading dimensions in elements; any alignment beyond that is served (rows at multiples of 128 bytes are the fastest).
  *
  * These calls launch kernels on `stream` and return, like gcoo_spdm(): they wait for nothing, allocate nothing, copy nothing back and may be recorded into a
@@ -337,7 +339,7 @@ int gcoo_spdm_epilogue(const gcoo_matrix* A, const void* B_dev, int64_t ldb, int
  *   dC_dev    m x N, lddc >= N: the gradient of C, which is the gradient of the residual as well
  *   dZ_dev    m x N, lddz >= N, or NULL where only dbias is wanted; may be dC itself (then lddz == lddc) or Z itself (lddz == ldz)
  *   dbias_dev m, or NULL
- * relu has the slope 0 at 0; where Z is infinite every slope is 0 or 1, to 2^-60.  m = 0 is a no-op success, N = 0 gives dbias = 0.
+ * relu has the slope 0 at 0; where Z is infinite every slope is 0 or 1.  m = 0 is a no-op success, N = 0 gives dbias = 0.
  */
 size_t gcoo_epilogue_grad_bytes(int64_t m, int64_t N);
 int gcoo_epilogue_grad(int64_t m, int64_t N, int type, int activation, const void* Z_dev, int64_t ldz, const void* dC_dev, int64_t lddc,

@@ -96,12 +96,23 @@ __device__ __forceinline__ void activate_all(int act, float (&z)[N])
     else { GCOO_EACH(GCOO_ACT_GELU_TANH) }
 #undef GCOO_EACH
 }
-// (z s(q z + r z^3))' at z, s the logistic function: s + z s (1 - s) (q + 3 r z^2).  1 - s is E s, E = exp(-(q z + r z^3)): the difference would have lost what the factors behind it
-// need.  `c` is z held where E is finite; what is left out there is below 1e-18.
-__device__ __forceinline__ float slope_of_gate(float z, float c, float q, float r)
+// (z s(x))' at z, x = q z + r z^3, s the logistic function: s(x) + z s(x) s(-x) (q + 3 r z^2).  s(-|x|) is E s(|x|), E = exp(-|x|): a difference would lose what the factors behind it need, and E has no end that z would
+// have to be held in front of.  (z is held at 16 or 256 all the same, where E is 0 in either form: infinite z gives 0 or 1.)
+template <typename T, bool CUBIC>
+__device__ __forceinline__ float slope_of_gate(float z)
 {
-    const float c2 = c * c, e = __expf(-c * (q + r * c2)), s = __builtin_amdgcn_rcpf(1.0f + e);
-    return z != z ? z : s + c * s * (e * s) * (q + 3.0f * r * c2);
+    constexpr float q = CUBIC ? 2.0f * kGeluA : 1.0f, r = CUBIC ? 2.0f * kGeluA * kGeluB : 0.0f, most = CUBIC ? 16.0f : 256.0f;
+    const float c = fminf(fmaxf(z, -most), most), c2 = c * c, x = fabsf(c * (q + r * c2));
+    float e, s;
+    if constexpr (sizeof(T) == 2) {
+        e = __expf(-x);
+        s = __builtin_amdgcn_rcpf(1.0f + e);
+    } else {
+        e = exp_below(-x);
+        s = reciprocal(1.0f + e);
+    }
+    const float small = e * s;
+    return z != z ? z : __builtin_fmaf(c * s, small * (q + 3.0f * r * c2), z < 0.0f ? small : s);
 }
 // dC act'(z)
 template <typename T>
@@ -109,14 +120,14 @@ __device__ __forceinline__ float slope_times(int act, float z, float d)
 {
     switch (act) {
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : d;
-        case GCOO_ACT_SILU: return slope_of_gate(z, fminf(fmaxf(z, -80.0f), 80.0f), 1.0f, 0.0f) * d;
+        case GCOO_ACT_SILU: return slope_of_gate<T, false>(z) * d;
         case GCOO_ACT_GELU: {
             // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi), which for a and -a add up to 1
             const GaussTail g = gauss_tail<T>(z);
             const float w = g.e * __builtin_fmaf(-kDensity0, g.a, g.q);
             return d * (z != z ? z : (z < 0.0f ? w : 1.0f - w));
         }
-        case GCOO_ACT_GELU_TANH: return slope_of_gate(z, fminf(fmaxf(z, -8.0f), 8.0f), 2.0f * kGeluA, 2.0f * kGeluA * kGeluB) * d;
+        case GCOO_ACT_GELU_TANH: return slope_of_gate<T, true>(z) * d;
         default: return d;
     }
 }

@@ -3,7 +3,8 @@
 How far they may be off, u = 2^-24.  With x the exponent that an activation takes (silu z, gelu z^2 / 2, gelu_tanh 2 sqrt(2 / pi) (z + 0.044715 z^3)), the exponential and at most sixteen roundings around it are off by
 16 u of the value.  An exponent formed in fp32 is off by as many u of itself as it has roundings, which the exponential turns into as many |x| u of its value: gelu_tanh has five (two of constants), gelu none in fp32, where
 what the square loses is not left out, and one for the types of 2 bytes.  Those have an exponential of a product and a power of two, 1.5 |x| u more, and a polynomial for gelu that is off by 2^-22.  An exponential
-below 2^-126, which is no normal number, may be 0: times z, that is up to 110, less than 2^-119.  A slope is a sum of two terms of either sign: the bound is of their magnitudes.  The rounding to the type comes on top."""
+below 2^-126, which is no normal number, may be 0: times z, that is up to 110, less than 2^-119 (and times z (2u)' = 244 where gelu_tanh's
+exponent 2u comes to that, at z = -10.2, less than 2^-118).  A slope is a sum of two terms of either sign: the bound is of their magnitudes.  The rounding to the type comes on top."""
 import math
 
 import numpy as np
@@ -64,7 +65,7 @@ def check(act, T, points, slopes=True):
     if not slopes:
         return
     want, both = slope(act, z64)
-    ref.check(binding.gcoo_epilogue_grad(torch.ones_like(z), Z=z, activation=act)[0], want, rel * both + U * (np.abs(want) + rel * both) + least, "slope")
+    ref.check(binding.gcoo_epilogue_grad(torch.ones_like(z), Z=z, activation=act)[0], want, rel * both + U * (np.abs(want) + rel * both) + least + 2.0 ** -119, "slope")
 
 
 GRID = np.linspace(-12.0, 12.0, 4801)
@@ -84,3 +85,15 @@ def test_gelu_in_16_bits(dtype):
 def test_silu_and_gelu_tanh_in_32_bits():
     check("silu", torch.float32, np.linspace(-80.0, 80.0, 40001), slopes=False)
     check("gelu_tanh", torch.float32, GRID, slopes=False)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_gates_far_out(act, dtype):
+    """Where the exponential is far from 1, the slope is not what it is at some nearer z."""
+    check(act, TYPES[dtype], np.concatenate([np.linspace(-110.0, -70.0, 801), GRID, np.linspace(70.0, 110.0, 801)]))
+
+
+def test_slopes_of_gates_in_32_bits():
+    check("silu", torch.float32, np.linspace(-80.0, 80.0, 40001))
+    check("gelu_tanh", torch.float32, GRID)
