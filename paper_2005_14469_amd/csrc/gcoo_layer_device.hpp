@@ -46,28 +46,28 @@ __device__ __forceinline__ float logistic(float x)
 }
 constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f, kDensity0 = 0.3989422804014327f;
 
-// Phi(-a) / exp(-a^2 / 2) and exp(-a^2 / 2), a = |z|, held where the exponential is 0 already (which it is where it is no normal number: what follows would go on with the few bits that are left of it): from these two
+// Phi(-a) / exp(-a^2 / 2) and exp(-a^2 / 2), a = |z| (where it is more than 16 the exponential is 0, and is so where it is no normal number: what follows would go on with the few bits that are left of it): from these two
 // come Phi(z) = 1 - Phi(-z) and the slope of gelu without a difference that would lose what is left of either for negative z.  The quotient falls slowly, like 1 / (a sqrt(2 pi)): t P(t), t = 1 / (1 + p a), P the
 // polynomial whose largest relative error over 0 <= a <= 16 is the least that its degree allows (by Remez' exchange, against the function in 64 bits).
 //   fp32: of degree 8, 2.4e-8, evaluated in fp32 6.3 2^-24.  What the square loses by rounding goes into the exponential as a factor: 2^-24 of an exponent of 72 would be 36 units of the result.
 //   T of 2 bytes: of degree 7, 1.7e-7, with the exponential and the reciprocal of single instructions: off by (2.5 s + 16) 2^-24 of the value, s the exponent, 2^-16 at z = -14, where half a step of bf16 is between 2^-9 and 2^-8.
-struct GaussTail { float q, e, a; };
+struct GaussTail { float q, e; };
 template <typename T>
-__device__ __forceinline__ GaussTail gauss_tail(float z)
+__device__ __forceinline__ GaussTail gauss_tail(float a)
 {
-    const float a = fminf(fabsf(z), 16.0f);
     if constexpr (sizeof(T) == 2) {
         const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.31f, a, 1.0f));
         float p = 0.0359124206f;
         p = __builtin_fmaf(p, t, -0.141914681f); p = __builtin_fmaf(p, t, 0.155632943f); p = __builtin_fmaf(p, t, -0.0154560292f); p = __builtin_fmaf(p, t, 0.110422157f);
         p = __builtin_fmaf(p, t, 0.107669815f); p = __builtin_fmaf(p, t, 0.12407776f); p = __builtin_fmaf(p, t, 0.123655692f);
-        return {p * t, __builtin_amdgcn_exp2f(a * a * -0.72134752f), a};            // -log2(e) / 2
+        return {p * t, __builtin_amdgcn_exp2f(a * a * -0.72134752f)};            // -log2(e) / 2
     }
+    a = fminf(a, 16.0f);
     const float s = a * a, lost = __builtin_fmaf(a, a, -s), t = reciprocal(__builtin_fmaf(0.27f, a, 1.0f));
     float p = 0.0290386342f;
     p = __builtin_fmaf(p, t, -0.126874849f); p = __builtin_fmaf(p, t, 0.170617849f); p = __builtin_fmaf(p, t, -0.0701981857f); p = __builtin_fmaf(p, t, 0.108535729f);
     p = __builtin_fmaf(p, t, 0.0717337355f); p = __builtin_fmaf(p, t, 0.101895243f); p = __builtin_fmaf(p, t, 0.107530423f); p = __builtin_fmaf(p, t, 0.107721426f);
-    return {p * t, exp_below(-0.5f * s, -0.5f * lost), a};
+    return {p * t, exp_below(-0.5f * s, -0.5f * lost)};
 }
 
 template <typename T>
@@ -77,8 +77,10 @@ __device__ __forceinline__ float activate(int act, float z)
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : z;
         case GCOO_ACT_SILU: return z * logistic<T>(z);
         case GCOO_ACT_GELU: {
-            const GaussTail g = gauss_tail<T>(z);
-            return __builtin_fmaf(-g.a, g.q * g.e, z <= 0.0f ? 0.0f : z);             // max(z, 0) - |z| Phi(-|z|)
+            // max(z, 0) - |z| Phi(-|z|); as z Phi(z), infinite where z is, and no number where z is -infinite
+            const float a = fabsf(fminf(z, 16.0f));
+            const GaussTail g = gauss_tail<T>(a);
+            return __builtin_fmaf(-a, g.q * g.e, z <= 0.0f ? 0.0f : z);
         }
         case GCOO_ACT_GELU_TANH: return z * logistic<T>(2.0f * kGeluA * (z + kGeluB * z * z * z));
         default: return z;
@@ -123,8 +125,9 @@ __device__ __forceinline__ float slope_times(int act, float z, float d)
         case GCOO_ACT_SILU: return slope_of_gate<T, false>(z) * d;
         case GCOO_ACT_GELU: {
             // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi), which for a and -a add up to 1
-            const GaussTail g = gauss_tail<T>(z);
-            const float w = g.e * __builtin_fmaf(-kDensity0, g.a, g.q);
+            const float a = fminf(fabsf(z), 16.0f);
+            const GaussTail g = gauss_tail<T>(a);
+            const float w = g.e * __builtin_fmaf(-kDensity0, a, g.q);
             return d * (z != z ? z : (z < 0.0f ? w : 1.0f - w));
         }
         case GCOO_ACT_GELU_TANH: return slope_of_gate<T, true>(z) * d;

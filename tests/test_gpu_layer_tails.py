@@ -97,3 +97,15 @@ def test_gates_far_out(act, dtype):
 def test_slopes_of_gates_in_32_bits():
     check("silu", torch.float32, np.linspace(-80.0, 80.0, 40001))
     check("gelu_tanh", torch.float32, GRID)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_of_infinite_sums(dtype):
+    """As the formulas have it: infinite on the right, -infinity times 0 on the left but for relu; very large finite sums give 0 there."""
+    big = 60000.0 if dtype == "f16" else 3e38
+    z = torch.tensor([[-math.inf, -big, big, math.inf, math.nan]], device=DEV, dtype=TYPES[dtype])
+    one = binding.gcoo_from_csr(1, 1, *[torch.from_numpy(a).to(DEV) for a in (np.array([0, 1], np.int32), np.zeros(1, np.int32), np.ones(1, np.float32))], 32, known_nnz=True)
+    for act in ("relu", "silu", "gelu", "gelu_tanh"):
+        y = binding.gcoo_spdm_epilogue(one, z, activation=act)[0]
+        assert torch.isnan(y[4]) and torch.equal(y[1:4], torch.stack([torch.zeros_like(z[0, 0]), z[0, 2], z[0, 3]])), (act, y)
+        assert y[0] == 0 if act == "relu" else torch.isnan(y[0]), (act, y)
