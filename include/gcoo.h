@@ -366,7 +366,7 @@ typedef struct gcoo_gradient {
 
 /*
  * norm = sqrt(the sum of the squares of all elements of all tensors); out = data x min(1, max_norm / (norm + 1e-6)).
- * Squares and their sums are held in 64 bits.  Where the factor is 1, tensors in place are left as they are.  Elements that are not finite make the norm
+ * Squares and their sums are held in 64 bits, and so is what the factor takes of them: a norm that fp32 has no number for is stored as infinite, but scales as any other.  Where the factor is 1, tensors in place are left as they are.  Elements that are not finite make the norm
  * not finite: an infinite one makes the factor 0, NaN makes every element NaN.  max_norm = INFINITY (or above any norm) copies what is not in place.
  *   list      `tensors` of them in HOST memory, read before the call returns; a range of `out` may overlap no range of another tensor, nor its own `data` but
  *             as data itself (GCOO_EINVAL)

@@ -99,8 +99,8 @@ __global__ __launch_bounds__(kClipThreads) void clip_sum(ClipList l, double* sum
 }
 
 // (x may be y: a thread loads what it stores itself)
-template <int THREADS, typename T>
-__device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t first, int n, float factor, int t)
+template <int THREADS, typename T, typename F>
+__device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t first, int n, F factor, int t)
 {
     constexpr int V = kClipVec<T>;
     const T* x = static_cast<const T*>(data) + first;
@@ -118,7 +118,7 @@ __device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t
     for (int s = 0; s < kClipSteps<T, THREADS>; ++s) {
         const int at = (s * THREADS + t) * V;
 #pragma unroll
-        for (int u = 0; u < V; ++u) v[s][u] *= factor;
+        for (int u = 0; u < V; ++u) v[s][u] = (float)(v[s][u] * factor);
         if (at + V <= n) layer_store<T, V>(y, at, v[s]);
         else
 #pragma unroll
@@ -127,22 +127,36 @@ __device__ __forceinline__ void clip_scaled(const void* data, void* out, int64_t
     }
 }
 
-// What the norm of all says is to be done.
+// What the norm of all says is to be done.  Finite elements may have a norm that fp32 has no number for, or a factor that it has none for, or one of few bits: then, which is seldom, both are in 64 bits (`wide`).
 struct ClipFactor {
-    bool scales;
+    bool scales, wide;
     float f;
-    __device__ __forceinline__ ClipFactor(float norm, float max_norm)
+    double norm, max_norm;
+    __device__ __forceinline__ ClipFactor(double norm64, float most) : norm(norm64), max_norm(most)
     {
-        scales = !(max_norm >= norm + 1e-6f);                       // (a NaN scales)
-        f = scales ? max_norm / (norm + 1e-6f) : 1.0f;
+        const float n = (float)norm64;
+        scales = !(most >= n + 1e-6f);                              // (a NaN scales)
+        f = scales ? most / (n + 1e-6f) : 1.0f;
+        wide = scales && f < 0x1p-100f && most > 0.0f && norm64 < (double)INFINITY;
     }
-    template <int THREADS>
-    __device__ __forceinline__ void apply(const ClipTensor& t, int64_t at, int n, int thread) const
+    template <int THREADS, typename F>
+    __device__ __forceinline__ void apply(const ClipTensor& t, int64_t at, int n, F factor, int thread) const
     {
         if (!scales && t.data == t.out) return;
-        if (t.type == GCOO_F32) clip_scaled<THREADS, float>(t.data, t.out, at, n, f, thread);
-        else if (t.type == GCOO_BF16) clip_scaled<THREADS, bf16_t>(t.data, t.out, at, n, f, thread);
-        else clip_scaled<THREADS, f16_t>(t.data, t.out, at, n, f, thread);
+        if (t.type == GCOO_F32) clip_scaled<THREADS, float>(t.data, t.out, at, n, factor, thread);
+        else if (t.type == GCOO_BF16) clip_scaled<THREADS, bf16_t>(t.data, t.out, at, n, factor, thread);
+        else clip_scaled<THREADS, f16_t>(t.data, t.out, at, n, factor, thread);
+    }
+    // each(g): g(tensor, first element, elements) for what the thread has a part in
+    template <int THREADS, typename E>
+    __device__ __forceinline__ void all(int thread, E&& each) const
+    {
+        if (__builtin_expect(wide, 0)) {
+            const double factor = max_norm / (norm + 1e-6);
+            each([&](const ClipTensor& t, int64_t at, int n) { apply<THREADS>(t, at, n, factor, thread); });
+        } else {
+            each([&](const ClipTensor& t, int64_t at, int n) { apply<THREADS>(t, at, n, f, thread); });
+        }
     }
 };
 
@@ -151,10 +165,9 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale(ClipList l, const dou
     __shared__ double part[kClipThreads / 64];
     double sum = 0.0;
     for (int32_t i = threadIdx.x; i < sums_all; i += kClipThreads) sum += sums[i];
-    const float norm = (float)sqrt(clip_block_sum<kClipThreads / 64>(sum, part));
-    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
-    const ClipFactor factor(norm, max_norm);
-    clip_pieces<true>(l, [&](const ClipTensor& t, int64_t at, int n) { factor.apply<kClipThreads>(t, at, n, (int)threadIdx.x); });
+    const double norm = sqrt(clip_block_sum<kClipThreads / 64>(sum, part));
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    ClipFactor(norm, max_norm).all<kClipThreads>((int)threadIdx.x, [&](auto&& f) { clip_pieces<true>(l, f); });
 }
 
 // A few pieces: one workgroup, whose quarters take a stretch each, and one launch (us, two launches and so, fp32: 2000 elements: 7.3 5.5; 16384: 6.6 5.4; 24576: 6.7 6.5; 49152: 6.9 9.3).
@@ -166,10 +179,9 @@ __global__ __launch_bounds__(kClipSmallThreads) void clip_small(ClipList l, floa
     const int32_t from = l.pieces * group / GROUPS, to = l.pieces * (group + 1) / GROUPS;
     double sum = 0.0;
     clip_stretch<false>(l, from, to, [&](const ClipTensor& x, int64_t at, int n) { sum += clip_squares_of<kClipThreads>(x, at, n, t); });
-    const float norm = (float)sqrt(clip_block_sum<kClipSmallThreads / 64>(sum, part));
-    if (threadIdx.x == 0) *norm_out = norm;
-    const ClipFactor factor(norm, max_norm);
-    clip_stretch<true>(l, from, to, [&](const ClipTensor& x, int64_t at, int n) { factor.apply<kClipThreads>(x, at, n, t); });
+    const double norm = sqrt(clip_block_sum<kClipSmallThreads / 64>(sum, part));
+    if (threadIdx.x == 0) *norm_out = (float)norm;
+    ClipFactor(norm, max_norm).all<kClipThreads>(t, [&](auto&& f) { clip_stretch<true>(l, from, to, f); });
 }
 
 hipError_t launch_clip_small(const ClipList& l, float max_norm, float* norm_out, hipStream_t s)
