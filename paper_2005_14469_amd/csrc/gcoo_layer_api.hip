@@ -104,7 +104,7 @@ ValuesWork values_work(const gcoo::RowsView& A, const gcoo::ValuesPlan& p, int t
 {
     ValuesWork w;
     w.part = aligned((size_t)p.starts * 4);
-    w.copy = w.part + (p.parts > 1 ? aligned((size_t)p.parts * (size_t)A.nnz * 4) : 0);
+    w.copy = w.part + (p.parts > 1 ? aligned((size_t)p.group * (size_t)A.nnz * 4) : 0);
     w.total = w.copy + aligned((size_t)A.k * (size_t)p.ldw * gcoo::type_bytes(type));
     return w;
 }

@@ -4,6 +4,8 @@
 #include "gcoo_layer_long.hpp"
 #include "gcoo_spdm_rows_kernel.hpp"
 
+#include <algorithm>
+
 namespace gcoo {
 
 // ---- from the caches: entry by entry ----
@@ -153,10 +155,11 @@ struct ValuesTile {
     uint32_t kmax, pitch;
     int64_t j0;
     int lane;
-    __device__ __forceinline__ ValuesTile(const GradValuesArgs& args, int32_t tile, float* part) : a(args)
+    // `tile` of a launch whose first one is `tile0`
+    __device__ __forceinline__ ValuesTile(const GradValuesArgs& args, int32_t tile0, int32_t tile, float* part) : a(args)
     {
         lane = threadIdx.x & 63;
-        j0 = (int64_t)tile * (16 * P * E);
+        j0 = (int64_t)(tile0 + tile) * (16 * P * E);
         out = part ? part + (int64_t)tile * a.A.nnz : a.dvals;
         const int64_t N = a.N;
         // (a tile of fewer than E columns begins E in front of N: N is at least E)
@@ -273,7 +276,7 @@ struct ValuesTile {
 };
 
 template <typename T, int P, bool ANY>
-__global__ __launch_bounds__(kValuesThreads) void values_entries(GradValuesArgs a, float* part, int32_t tiles, int32_t row_wgs, int32_t one)
+__global__ __launch_bounds__(kValuesThreads) void values_entries(GradValuesArgs a, float* part, int32_t tile0, int32_t tiles, int32_t row_wgs, int32_t one)
 {
     // an XCD walks all rows of one tile before the next, eight tiles side by side; the tiles beyond the last whole eight are cut into eight slices of rows
     const int32_t block = (int32_t)blockIdx.x, xcd = block & 7, at = block >> 3, eights = tiles / 8;
@@ -299,8 +302,8 @@ __global__ __launch_bounds__(kValuesThreads) void values_entries(GradValuesArgs 
         while (walk.next(&row, &piece)) t.long_row(row, piece);
         if (r0 < a.A.m) t.rows(r0, one, beg, end);
     };
-    if ((int64_t)(tile + 1) * (16 * P * Piece<T>::kElements) > a.N) work(ValuesTile<T, P, true, ANY>(a, tile, part));
-    else work(ValuesTile<T, P, false, ANY>(a, tile, part));
+    if ((int64_t)(tile0 + tile + 1) * (16 * P * Piece<T>::kElements) > a.N) work(ValuesTile<T, P, true, ANY>(a, tile0, tile, part));
+    else work(ValuesTile<T, P, false, ANY>(a, tile0, tile, part));
 }
 
 // ---- few columns: a lane per entry ----
@@ -539,15 +542,23 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void values_tiles(GradValuesArgs a
     }
 }
 
-// ---- dvals[e] = the sums of the tiles or parts, in their order ----
+// ---- dvals[e] = the sums of the tiles or parts, in their order; MORE: behind what it holds ----
+template <bool MORE>
 __global__ __launch_bounds__(kValuesThreads) void values_join(const float* __restrict__ part, float* __restrict__ dvals, int64_t nnz, int32_t parts)
 {
     const int64_t e = (int64_t)blockIdx.x * kValuesThreads + threadIdx.x;
     if (e >= nnz) return;
     float s = part[e];
+    if (MORE) s += dvals[e];
 #pragma unroll 8
     for (int32_t i = 1; i < parts; ++i) s += part[(int64_t)i * nnz + e];
     dvals[e] = s;
+}
+static hipError_t launch_join(const float* part, float* dvals, int64_t nnz, int32_t parts, bool more, hipStream_t s)
+{
+    const auto kernel = more ? values_join<true> : values_join<false>;
+    kernel<<<dim3((unsigned)((nnz + kValuesThreads - 1) / kValuesThreads)), dim3(kValuesThreads), 0, s>>>(part, dvals, nnz, parts);
+    return hipGetLastError();
 }
 
 // ---- launches ----
@@ -556,12 +567,17 @@ template <typename T, int P>
 static hipError_t launch_entries(const GradValuesArgs& a, const ValuesPlan& plan, float* part, hipStream_t s)
 {
     constexpr int64_t waves = kValuesThreads / 64;
-    const int64_t rows = plan.one ? waves : 4 * waves, row_wgs = (a.A.m + rows - 1) / rows, tiles = plan.parts;
-    const int64_t rest = tiles % 8 * row_wgs, grid = tiles / 8 * 8 * row_wgs + (rest + 7) / 8 * 8;
-    if (too_wide(grid, kValuesThreads)) return hipErrorInvalidConfiguration;
+    const int64_t rows = plan.one ? waves : 4 * waves, row_wgs = (a.A.m + rows - 1) / rows;
     const auto kernel = plan.any ? values_entries<T, P, true> : values_entries<T, P, false>;
-    kernel<<<dim3((unsigned)grid), dim3(kValuesThreads), 0, s>>>(a, tiles > 1 ? part : nullptr, (int32_t)tiles, (int32_t)row_wgs, plan.one ? 1 : 0);
-    return hipGetLastError();
+    for (int32_t tile0 = 0; tile0 < plan.parts; tile0 += plan.group) {
+        const int64_t tiles = plan.parts - tile0 < plan.group ? plan.parts - tile0 : plan.group, rest = tiles % 8 * row_wgs, grid = tiles / 8 * 8 * row_wgs + (rest + 7) / 8 * 8;
+        if (too_wide(grid, kValuesThreads)) return hipErrorInvalidConfiguration;
+        kernel<<<dim3((unsigned)grid), dim3(kValuesThreads), 0, s>>>(a, plan.parts > 1 ? part : nullptr, tile0, (int32_t)tiles, (int32_t)row_wgs, plan.one ? 1 : 0);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && plan.parts > 1) e = launch_join(part, a.dvals, a.A.nnz, (int32_t)tiles, tile0 > 0, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T>
@@ -591,7 +607,8 @@ static hipError_t launch_tiles(const GradValuesArgs& a, const ValuesPlan& plan, 
     values_starts<<<dim3((unsigned)((a.A.m + kValuesThreads / 64 - 1) / (kValuesThreads / 64))), dim3(kValuesThreads), 0, s>>>(a.A, (int32_t)tiles_n, TN, starts);
     kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WM * WN), lds, s>>>(a, starts, plan.parts > 1 ? part : a.dvals, (int32_t)tiles_m, (int32_t)tiles_n, plan.parts,
                                                                                    (int32_t)((steps + plan.parts - 1) / plan.parts));
-    return hipGetLastError();
+    const hipError_t launched = hipGetLastError();
+    return launched != hipSuccess || plan.parts == 1 ? launched : launch_join(part, a.dvals, a.A.nnz, plan.parts, false, s);
 }
 
 // Times of the two kernels, in microseconds, of which the shorter is taken.  Entries: what they take of B through the vector caches, both matrices from memory once.  Tiles: all products of
@@ -608,7 +625,7 @@ static double tiles_time(double m, double k, double nnz, double N, int type)
 ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, const void* B, int64_t ldb)
 {
     const int64_t size = (int64_t)type_bytes(type), bytes = N * size;
-    ValuesPlan p{kValuesFew, 1, 1, false, false, 0, 0};
+    ValuesPlan p{kValuesFew, 1, 1, 1, false, false, 0, 0};
     // (from eight columns on a slot of 16 lanes takes 16 bytes a lane and nothing beside them; us, a lane per entry and so: bf16, 8000 x 8000, 5 %, N = 8: 40 38, 16: 71 39, 32: 213 38; 0.5 %, N = 32: 43 10; fp32, 5 %,
     // N = 4: 27 35, 8: 42 35, 16: 110 35; power-law rows, 16384 x 16384, of 53, bf16, N = 8: 41 36, 32: 136 35)
     if (N < 8) return p;
@@ -627,7 +644,7 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
         p.pieces = type != GCOO_F32 && ((m + 255) / 256) * ((k + 255) / 256) >= 160 ? 4 : 2;
         const int64_t edge = values_tile_cols(p.pieces == 4), tiles_n = (k + edge - 1) / edge, tiles = ((m + edge - 1) / edge) * tiles_n, steps = (bytes + 127) / 128;
         const int64_t wanted = p.pieces == 4 ? 1 : (512 + tiles - 1) / tiles, most = (steps + 3) / 4, parts = wanted < most ? wanted : most, each = (steps + parts - 1) / parts;
-        p.parts = (int32_t)((steps + each - 1) / each);                    // none of them empty
+        p.parts = p.group = (int32_t)((steps + each - 1) / each);          // none of them empty
         p.starts = m * (tiles_n + 1);
         return p;
     }
@@ -641,6 +658,11 @@ ValuesPlan values_plan(int64_t m, int64_t k, int64_t nnz, int64_t N, int type, c
     if (bytes <= 1024) p.pieces = bytes <= 256 ? 1 : (bytes <= 512 ? 2 : 4);
     else p.pieces = k <= 3500 ? 4 : (k <= 10000 ? 2 : 1);
     p.parts = (int32_t)((bytes + 256 * p.pieces - 1) / (256 * p.pieces));
+    // As many tiles to a launch as leave kValuesSums of their sums, but eight at the least, one to an XCD; all of about the same number.  (A launch more costs the end of one, where workgroups of long rows are alone: us, fp32,
+    // one launch, 1 GB and 256 MB of sums: 14000 x 14000, 16.7 million entries, N = 2653: 7638 7758 8132; 5.9 million, N = 8000: 8663 8716 8934; 12000 x 12000, 4 %, N = 8000: 8034 8188 8370.  The sums would grow with
+    // N: 3 GB for the first two.)
+    const int64_t most = std::max<int64_t>(kValuesSums / nnz / 8 * 8, 8), launches = (p.parts + most - 1) / most;
+    p.group = launches > 1 ? (int32_t)(((p.parts + launches - 1) / launches + 7) / 8 * 8) : p.parts;
     p.one = m * p.parts < 4096 && nnz >= 12 * m;
     return p;
 }
@@ -656,7 +678,7 @@ hipError_t launch_grad_values(const GradValuesArgs& args, const ValuesPlan& plan
         a.B = copy;
         a.ldb = plan.ldw;
     }
-    e = with_type(a.type, [&](auto t) {
+    return with_type(a.type, [&](auto t) {
         typedef decltype(t) T;
         if (plan.kernel == kValuesFew) return launch_few<T>(a, s);
         if (plan.kernel == kValuesTiles) {
@@ -666,9 +688,6 @@ hipError_t launch_grad_values(const GradValuesArgs& args, const ValuesPlan& plan
         }
         return plan.pieces == 1 ? launch_entries<T, 1>(a, plan, part, s) : (plan.pieces == 2 ? launch_entries<T, 2>(a, plan, part, s) : launch_entries<T, 4>(a, plan, part, s));
     });
-    if (e != hipSuccess || plan.parts == 1) return e;
-    values_join<<<dim3((unsigned)((a.A.nnz + kValuesThreads - 1) / kValuesThreads)), dim3(kValuesThreads), 0, s>>>(part, a.dvals, a.A.nnz, plan.parts);
-    return hipGetLastError();
 }
 
 }  // namespace gcoo
