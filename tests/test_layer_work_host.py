@@ -12,7 +12,7 @@ def stub():
     host_calls.build()
 
 
-@pytest.mark.parametrize("case", ["bounds"])
+@pytest.mark.parametrize("case", ["bounds", "too_little", "groups"])
 def test_host_code(case):
     r = subprocess.run([sys.executable, "-m", "tests.layer_work_calls", case], cwd=host_calls.ROOT, capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and r.stdout.endswith("ok\n"), r.stdout + r.stderr
