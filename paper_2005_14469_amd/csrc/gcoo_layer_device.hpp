@@ -23,33 +23,64 @@ auto with_type(int type, F&& f)
 }
 
 // exp(x + more) for x <= 0, `more` a remainder that x is too coarse to hold: the instruction's power of two, off by a unit in the last place, times what the exponent loses by rounding; 0 below 2^-126, where
-// the instruction has no numbers.  (The library's expf, which has them, takes more than twice as many instructions.)
+// the instruction has no numbers.  (With the library's expf, which has them, and a quotient the product with gelu, 1777 x 2301, 3 %, N = 1117, fp32, took 24.3 us, so 23.9.)
 __device__ __forceinline__ float exp_below(float x, float more = 0.0f)
 {
     constexpr float hi = 1.44269502f, lo = 1.92596299e-8f, ln2 = 0.693147182f;              // hi + lo = 1 / ln 2
     const float c = fmaxf(x, -200.0f), h = c * hi, e = __builtin_amdgcn_exp2f(h);
     return __builtin_fmaf(e, __builtin_fmaf(ln2, __builtin_fmaf(c, lo, __builtin_fmaf(c, hi, -h)), more), e);
 }
-// 1 / x for x >= 1, off by less than a unit in the last place: the instruction's and one step of Newton's.
-__device__ __forceinline__ float reciprocal(float x)
+// 1 / (x + more) for x >= 1, `more` what x has lost by rounding: the instruction's and one step of Newton's, off by little more than half a unit in the last place.
+__device__ __forceinline__ float reciprocal(float x, float more = 0.0f)
 {
     const float r = __builtin_amdgcn_rcpf(x);
-    return __builtin_fmaf(__builtin_fmaf(-x, r, 1.0f), r, r);
+    return __builtin_fmaf(__builtin_fmaf(-more, r, __builtin_fmaf(-x, r, 1.0f)), r, r);
 }
-// 1 / (1 + exp(-x)).  In fp32 off by 8 2^-24, for negative x as exp(x) / (1 + exp(x)); for types of 2 bytes by single instructions, (1.5 |x| + 2) 2^-24.
+// s(x) = 1 / (1 + exp(-x)) and s(-x) of x >= 0.  In fp32 off by 8 2^-24; for types of 2 bytes by single instructions, (1.5 x + 2) 2^-24.
+struct Logistic { float s, tail; };
 template <typename T>
-__device__ __forceinline__ float logistic(float x)
+__device__ __forceinline__ Logistic logistic(float x)
 {
-    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_rcpf(1.0f + __expf(-x));
-    const float e = exp_below(-fabsf(x)), s = reciprocal(1.0f + e);
-    return x < 0.0f ? e * s : s;
+    if constexpr (sizeof(T) == 2) {
+        const float e = __expf(-x), s = __builtin_amdgcn_rcpf(1.0f + e);
+        return {s, e * s};
+    }
+    const float e = exp_below(-x), s = reciprocal(1.0f + e);
+    return {s, e * s};
 }
 constexpr float kGeluA = 0.7978845608028654f, kGeluB = 0.044715f, kDensity0 = 0.3989422804014327f;
+
+// silu and gelu_tanh are z s(x), x = q z + r z^3: max(z, 0) - |z| s(-|x|), whose slope is w for negative z and 1 - w else, w = s(-|x|) (1 - |z| s(|x|) (q + 3 r z^2)).  s(-|x|) as a difference would have lost what the factors
+// beside it need.
+template <bool CUBIC> struct Gate {
+    static constexpr float q = CUBIC ? 2.0f * kGeluA : 1.0f, r = CUBIC ? 2.0f * kGeluA * kGeluB : 0.0f;
+    static constexpr float most = CUBIC ? 16.0f : 256.0f;             // of |z|: beyond, the exponential is 0
+};
+template <typename T, bool CUBIC>
+__device__ __forceinline__ float gate(float z)
+{
+    typedef Gate<CUBIC> G;
+    if constexpr (sizeof(T) == 2) {
+        const float x = CUBIC ? 2.0f * kGeluA * (z + kGeluB * z * z * z) : z;
+        return z * __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+    }
+    const float a = fabsf(fminf(z, G::most));                         // (so it is infinite where z is, and, as z s(x), no number where z is -infinite)
+    return __builtin_fmaf(-a, logistic<T>(CUBIC ? a * (G::q + G::r * (a * a)) : a).tail, z <= 0.0f ? 0.0f : z);
+}
+template <typename T, bool CUBIC>
+__device__ __forceinline__ float gate_slope(float z)
+{
+    typedef Gate<CUBIC> G;
+    const float a = fminf(fabsf(z), G::most), a2 = a * a;
+    const Logistic l = logistic<T>(CUBIC ? a * (G::q + G::r * a2) : a);
+    const float w = l.tail * __builtin_fmaf(-a * l.s, CUBIC ? G::q + 3.0f * G::r * a2 : 1.0f, 1.0f);
+    return z != z ? z : (z < 0.0f ? w : 1.0f - w);
+}
 
 // Phi(-a) / exp(-a^2 / 2) and exp(-a^2 / 2), a = |z| (where it is more than 16 the exponential is 0, and is so where it is no normal number: what follows would go on with the few bits that are left of it): from these two
 // come Phi(z) = 1 - Phi(-z) and the slope of gelu without a difference that would lose what is left of either for negative z.  The quotient falls slowly, like 1 / (a sqrt(2 pi)): t P(t), t = 1 / (1 + p a), P the
 // polynomial whose largest relative error over 0 <= a <= 16 is the least that its degree allows (by Remez' exchange, against the function in 64 bits).
-//   fp32: of degree 8, 2.4e-8, evaluated in fp32 6.3 2^-24.  What the square loses by rounding goes into the exponential as a factor: 2^-24 of an exponent of 72 would be 36 units of the result.
+//   fp32: of degree 9, 1.6e-8, p = 0.4 and what 1 + p a loses by rounding given to its reciprocal, since the quotient changes by up to twice what t does.  What the square loses by rounding goes into the exponential as a factor: 2^-24 of an exponent of 72 would be 36 units of the result.
 //   T of 2 bytes: of degree 7, 1.7e-7, with the exponential and the reciprocal of single instructions: off by (2.5 s + 16) 2^-24 of the value, s the exponent, 2^-16 at z = -14, where half a step of bf16 is between 2^-9 and 2^-8.
 struct GaussTail { float q, e; };
 template <typename T>
@@ -63,10 +94,11 @@ __device__ __forceinline__ GaussTail gauss_tail(float a)
         return {p * t, __builtin_amdgcn_exp2f(a * a * -0.72134752f)};            // -log2(e) / 2
     }
     a = fminf(a, 16.0f);
-    const float s = a * a, lost = __builtin_fmaf(a, a, -s), t = reciprocal(__builtin_fmaf(0.27f, a, 1.0f));
-    float p = 0.0290386342f;
-    p = __builtin_fmaf(p, t, -0.126874849f); p = __builtin_fmaf(p, t, 0.170617849f); p = __builtin_fmaf(p, t, -0.0701981857f); p = __builtin_fmaf(p, t, 0.108535729f);
-    p = __builtin_fmaf(p, t, 0.0717337355f); p = __builtin_fmaf(p, t, 0.101895243f); p = __builtin_fmaf(p, t, 0.107530423f); p = __builtin_fmaf(p, t, 0.107721426f);
+    const float s = a * a, lost = __builtin_fmaf(a, a, -s), x = __builtin_fmaf(0.4f, a, 1.0f), t = reciprocal(x, __builtin_fmaf(0.4f, a, 1.0f - x));
+    float p = 0.0324279107f;
+    p = __builtin_fmaf(p, t, -0.177947655f); p = __builtin_fmaf(p, t, 0.384890705f); p = __builtin_fmaf(p, t, -0.377340198f); p = __builtin_fmaf(p, t, 0.122096606f);
+    p = __builtin_fmaf(p, t, -0.0281496216f); p = __builtin_fmaf(p, t, 0.0917519927f); p = __builtin_fmaf(p, t, 0.133058563f); p = __builtin_fmaf(p, t, 0.159636229f);
+    p = __builtin_fmaf(p, t, 0.159575492f);
     return {p * t, exp_below(-0.5f * s, -0.5f * lost)};
 }
 
@@ -75,14 +107,14 @@ __device__ __forceinline__ float activate(int act, float z)
 {
     switch (act) {
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : z;
-        case GCOO_ACT_SILU: return z * logistic<T>(z);
+        case GCOO_ACT_SILU: return gate<T, false>(z);
         case GCOO_ACT_GELU: {
             // max(z, 0) - |z| Phi(-|z|); as z Phi(z), infinite where z is, and no number where z is -infinite
             const float a = fabsf(fminf(z, 16.0f));
             const GaussTail g = gauss_tail<T>(a);
             return __builtin_fmaf(-a, g.q * g.e, z <= 0.0f ? 0.0f : z);
         }
-        case GCOO_ACT_GELU_TANH: return z * logistic<T>(2.0f * kGeluA * (z + kGeluB * z * z * z));
+        case GCOO_ACT_GELU_TANH: return gate<T, true>(z);
         default: return z;
     }
 }
@@ -98,31 +130,13 @@ __device__ __forceinline__ void activate_all(int act, float (&z)[N])
     else { GCOO_EACH(GCOO_ACT_GELU_TANH) }
 #undef GCOO_EACH
 }
-// (z s(x))' at z, x = q z + r z^3, s the logistic function: s(x) + z s(x) s(-x) (q + 3 r z^2).  s(-|x|) is E s(|x|), E = exp(-|x|): a difference would lose what the factors behind it need, and E has no end that z would
-// have to be held in front of.  (z is held at 16 or 256 all the same, where E is 0 in either form: infinite z gives 0 or 1.)
-template <typename T, bool CUBIC>
-__device__ __forceinline__ float slope_of_gate(float z)
-{
-    constexpr float q = CUBIC ? 2.0f * kGeluA : 1.0f, r = CUBIC ? 2.0f * kGeluA * kGeluB : 0.0f, most = CUBIC ? 16.0f : 256.0f;
-    const float c = fminf(fmaxf(z, -most), most), c2 = c * c, x = fabsf(c * (q + r * c2));
-    float e, s;
-    if constexpr (sizeof(T) == 2) {
-        e = __expf(-x);
-        s = __builtin_amdgcn_rcpf(1.0f + e);
-    } else {
-        e = exp_below(-x);
-        s = reciprocal(1.0f + e);
-    }
-    const float small = e * s;
-    return z != z ? z : __builtin_fmaf(c * s, small * (q + 3.0f * r * c2), z < 0.0f ? small : s);
-}
 // dC act'(z)
 template <typename T>
 __device__ __forceinline__ float slope_times(int act, float z, float d)
 {
     switch (act) {
         case GCOO_ACT_RELU: return z <= 0.0f ? 0.0f : d;
-        case GCOO_ACT_SILU: return slope_of_gate<T, false>(z) * d;
+        case GCOO_ACT_SILU: return gate_slope<T, false>(z) * d;
         case GCOO_ACT_GELU: {
             // Phi(z) + z exp(-z^2 / 2) / sqrt(2 pi), which for a and -a add up to 1
             const float a = fminf(fabsf(z), 16.0f);
@@ -130,7 +144,7 @@ __device__ __forceinline__ float slope_times(int act, float z, float d)
             const float w = g.e * __builtin_fmaf(-kDensity0, a, g.q);
             return d * (z != z ? z : (z < 0.0f ? w : 1.0f - w));
         }
-        case GCOO_ACT_GELU_TANH: return slope_of_gate<T, true>(z) * d;
+        case GCOO_ACT_GELU_TANH: return gate_slope<T, true>(z) * d;
         default: return d;
     }
 }
