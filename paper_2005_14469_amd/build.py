@@ -135,7 +135,7 @@ def verify_band_code(stem: str, text: str, name: str = "spdm_bandI") -> None:
         written, read = isa_check.asm_scalar_writes(text, kernel)
         if written != set(range(12, 32)) | set(range(36, 100)) | ({100} if v == 2 else set()) or not read:
             raise RuntimeError(f"{stem} {kernel}: scalar registers written {sorted(written)}, read {sorted(read)}")
-    # (beside them there is one for uneven rows, of ordinary code)
+    # (beside them there is one for uneven rows, of ordinary code, whose spills, 14 to 18 vector registers, are not looked at)
     kernels = text[text.index("amdhsa.kernels"):].split("  - .agpr_count")[1:]
     meta = "".join(x for x in kernels if "layer_rows_all" not in x)
     for key, most in (("vgpr_spill_count", 0), ("sgpr_spill_count", 0), ("private_segment_fixed_size", 0), ("vgpr_count", 128)):

@@ -1,6 +1,6 @@
 // The product with its epilogue row by row (gcoo_spdm_rows_kernel.hpp, with B in its own type and the epilogue in the place of the stores), and for few
 // columns; instances by type in layer_rows_*.hip.
-// Bound: the rows of B through the vector caches (8000 x 8000, 0.5 %, N = 8000, bf16, bias, gelu_tanh and residual: 297 us behind cold caches, 5.1 GB of rows of B, 18 TB/s; B, residual and C once would take 79).
+// Bound: the rows of B through the vector caches (8000 x 8000, 0.5 %, N = 8000, bf16, bias, gelu_tanh and residual: 296 us behind cold caches, 5.1 GB of rows of B, 18 TB/s; B, residual and C once would take 79).
 #pragma once
 #include "gcoo_layer_io.hpp"
 #include "gcoo_layer_long.hpp"

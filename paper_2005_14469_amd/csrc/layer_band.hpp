@@ -1,5 +1,5 @@
 // The sixteen-wave product with its epilogue: the kernel of gcoo_spdm_band_kernel.hpp, whose sums go through LDS to the epilogue; instances by type in layer_band_*.hip.
-// Bound: vector instructions, as without the epilogue (8000 x 8000, 10 %, N = 8000, fp32: 2010 us; with bias, gelu, residual and Z, 0.77 GB more: 2165).
+// Bound: vector instructions, as without the epilogue (8000 x 8000, 10 %, N = 8000, fp32: 2010 us; with bias, gelu, residual and Z, 0.77 GB more: 2171, the kernel alone 2145 to 2200 where pass follows pass).
 #pragma once
 #include "gcoo_layer_io.hpp"
 #include "gcoo_spdm_band_launch.hpp"
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(64 * kBandWaves) void layer_band(BandArgs a, RowsAr
     band_item<V, SPREAD, LATE, BandLayer<T>>(a, by_rows, rg, io);
 }
 
-// Uneven rows, one by one, in a launch of their own, of which nothing is left where there are none: with both in one kernel the scalar registers do not suffice.
+// Uneven rows, one by one, in a launch of their own, which ends at once where there are none (2 to 5 us): with both in one kernel the scalar registers do not suffice.  (128 vector registers, and 14 to 18 spilled.)
 template <typename T>
 __global__ __launch_bounds__(64 * kBandWaves) void layer_rows_all(const uint32_t* uneven, RowsArgs by_rows, BandRowsGrid rg, LayerIO<float, T> io)
 {

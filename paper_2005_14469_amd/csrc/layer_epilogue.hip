@@ -83,7 +83,7 @@ hipError_t launch_epilogue(int64_t m, int64_t N, const EpilogueArgs& e, hipStrea
 
 // The gradient through the epilogue: LANES lanes on a row (16, 64 or the 256 of a workgroup), each 16 bytes of it at a time, four such pieces of both operands on their way; the row's sum in a fixed tree.
 // Rows of a matrix that has few of them are cut into parts, a workgroup each, whose sums epilogue_grad_join adds in their order.
-// Bound: memory (14000 x 8000, bf16, silu: 118 us, 672 MB, 5.7 TB/s, where a large copy has 4.9: part of it is still in the memory-side cache); below a megabyte the launch (1000 x 333, fp32, gelu: 4.1 us in the kernel).
+// Bound: memory (14000 x 8000, bf16, silu: 119 us, 672 MB, 5.6 TB/s, where a large copy has 4.9: part of it is still in the memory-side cache); below a megabyte the launch (1000 x 333, fp32, gelu: 4.1 us in the kernel).
 template <typename T, int LANES>
 __global__ __launch_bounds__(kPassThreads) void layer_epilogue_grad(EpilogueGradArgs a, float* part, int64_t part_cols)
 {

@@ -16,7 +16,7 @@ namespace gcoo {
 // A wave has four rows beside each other, or all four slots on one row where it is long or rows are few.
 //
 // Bound: the vector caches, through which every entry takes its stretch of B.  The columns of B are cut into tiles of 256 P bytes that stay in an XCD's L2 (4 MB) for as many
-// rows as A has columns; the sums of a tile go to `work` and values_join adds them in the order of the tiles (8000 x 8000, 0.5 %, N = 8000, bf16: 287 us, 8 of it the joining; 5.1 GB of rows of B, 18 TB/s).
+// rows as A has columns; the sums of a tile go to `work` and values_join adds them in the order of the tiles (8000 x 8000, 0.5 %, N = 8000, bf16: 288 us, 8 of it the joining; 5.1 GB of rows of B, 18 TB/s).
 // Long rows are cut into pieces for whole workgroups, which take them first (us, power-law rows, 16384 x 16384, of 53 entries, N = 300: bf16 694 124, fp32 287 124; even rows up to 0.3 us more).
 constexpr int kLongPieces = 8;
 
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kValuesThreads) void values_few(GradValuesArgs a)
 // there to the matrix instructions by 16 bytes per lane.  Where those bytes lie in a step is the same for both operands, so the instructions may take them in any order.
 // 16 bytes of row r are at piece ^ (r / 2 mod 8) of its 128 in LDS: sixteen lanes that read one piece of sixteen rows, and sixteen that write two rows, meet all 64 banks once.
 // For few tiles N is cut into parts, whose sums are joined afterwards.
-// Bound: the matrix instructions (4001 x 3999, 5 %, N = 4003, bf16: 141 to 148 us with starts and join, 0.8 of the rate of a large product; 8000 x 8000, 10 %, N = 8000: bf16 1.0 ms, fp32 8.1 ms, 127 of 153 TFLOP/s).
+// Bound: the matrix instructions (4001 x 3999, 5 %, N = 4003, bf16: 142 us with the starts, 0.84 of the rate of a large product, and 150 to 185 where pass follows pass; 8000 x 8000, 10 %, N = 8000: bf16 1.0 ms, fp32 8.1 ms, 127 of 153 TFLOP/s).
 template <typename T> struct Mfma;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <> struct Mfma<bf16_t> {
