@@ -213,6 +213,6 @@ if __name__ == "__main__":
         rt = glob.glob("/opt/rocm/lib/llvm/lib/clang/*/lib/linux/libclang_rt.asan-x86_64.so")
         print(lib)
         print(f"run: GCOO_LIBRARY={lib} LD_PRELOAD={rt[0] if rt else '<libclang_rt.asan-x86_64.so>'} ASAN_OPTIONS=detect_leaks=0 "
-              "UBSAN_OPTIONS=halt_on_error=1 python -m pytest tests/test_abi_host.py tests/test_host_calls.py -q")
+              "UBSAN_OPTIONS=halt_on_error=1 python -m pytest tests/test_abi_host.py tests/test_host_calls.py tests/test_layer_host.py tests/test_layer_work_host.py -q")
     else:
         print(build())

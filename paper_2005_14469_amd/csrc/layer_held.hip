@@ -182,10 +182,9 @@ static hipError_t launch_held(const RowsArgs& a, const EpilogueArgs& e, hipStrea
     const int64_t grid = (wgs + 7) / 8 * 8 * tiles;
     if (tiles > 32 || too_wide(grid, kHeldThreads) || rows > INT32_MAX) return hipErrorInvalidConfiguration;
     static LdsLimit limit;
-    const auto kernel = &layer_held<T, LANES, N>;
-    const hipError_t err = limit.raise(reinterpret_cast<const void*>(kernel), (int)kHeldLdsBytes);
+    const hipError_t err = limit.raise(reinterpret_cast<const void*>(&layer_held<T, LANES, N>), (int)kHeldLdsBytes);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)grid), dim3(kHeldThreads), (size_t)lds, s>>>(a, e, (int32_t)tiles, (int32_t)wgs, (int32_t)rows);
+    layer_held<T, LANES, N><<<dim3((unsigned)grid), dim3(kHeldThreads), (size_t)lds, s>>>(a, e, (int32_t)tiles, (int32_t)wgs, (int32_t)rows);
     return hipGetLastError();
 }
 template <typename T, int LANES>

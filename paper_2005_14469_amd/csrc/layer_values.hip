@@ -597,15 +597,14 @@ static hipError_t launch_tiles(const GradValuesArgs& a, const ValuesPlan& plan, 
 {
     constexpr int TM = WM * MI * 32, TN = WN * 64, lds = 2 * (TM + TN) * 128;
     static_assert(64 * TN * 4 <= lds && TN == values_tile_cols(MI == 4), "the sums of 64 rows");
-    const auto kernel = &values_tiles<T, WM, WN, MI>;
     static LdsLimit limit;
-    const hipError_t e = limit.raise(reinterpret_cast<const void*>(kernel), lds);
+    const hipError_t e = limit.raise(reinterpret_cast<const void*>(&values_tiles<T, WM, WN, MI>), lds);
     if (e != hipSuccess) return e;
     const int64_t tiles_m = (a.A.m + TM - 1) / TM, tiles_n = (a.A.k + TN - 1) / TN, total = tiles_m * tiles_n * plan.parts;
     if (too_wide(total + 7, 64 * WM * WN) || too_wide((a.A.m + kValuesThreads / 64 - 1) / (kValuesThreads / 64), kValuesThreads)) return hipErrorInvalidConfiguration;
     const int64_t steps = (a.N * (int64_t)sizeof(T) + 127) / 128;
     values_starts<<<dim3((unsigned)((a.A.m + kValuesThreads / 64 - 1) / (kValuesThreads / 64))), dim3(kValuesThreads), 0, s>>>(a.A, (int32_t)tiles_n, TN, starts);
-    kernel<<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WM * WN), lds, s>>>(a, starts, plan.parts > 1 ? part : a.dvals, (int32_t)tiles_m, (int32_t)tiles_n, plan.parts,
+    values_tiles<T, WM, WN, MI><<<dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WM * WN), lds, s>>>(a, starts, plan.parts > 1 ? part : a.dvals, (int32_t)tiles_m, (int32_t)tiles_n, plan.parts,
                                                                                    (int32_t)((steps + plan.parts - 1) / plan.parts));
     const hipError_t launched = hipGetLastError();
     return launched != hipSuccess || plan.parts == 1 ? launched : launch_join(part, a.dvals, a.A.nnz, plan.parts, false, s);
